@@ -195,6 +195,130 @@ int varlen_attn_merge(const varlen_attn_params *p, int32_t num_parts, const void
 int varlen_attn_check_cu_seqlens(const varlen_attn_params *p, const int32_t *cu_seqlens, void *workspace,
                                  size_t workspace_bytes, void *hip_stream);
 
+/*
+ * What runs around attention in a block's training step, on the same packed tokens: rotary positions, layer norm, and
+ * checkpoints of activations in 8 bits.  All calls obey the contract at the top of this file (device pointers, nothing allocated
+ * or synchronised, capturable, every host-visible argument checked before anything is enqueued), except that their tensors need
+ * no more alignment than their elements have: rows that start on 16-byte boundaries and hold a multiple of 8 channels are moved 16
+ * bytes at a time, others element by element, with the same results.  Strides are in elements, from one token to the next, and a token's
+ * heads and channels lie side by side: a tensor may be a part of a wider one, such as q inside the fused projection
+ * [T, Hq + 2 Hkv, D].  Unless said otherwise no output may overlap an input or another output.
+ */
+
+/*
+ * The positions of a packed batch of text, images and video, on the axes time, height and width.
+ *   cu_rows    DEVICE int32 [num_segments + 1]: segment s holds the tokens [cu_rows[s], cu_rows[s + 1]); one sample may consist of
+ *              several segments (text, image, text)
+ *   grids      DEVICE int32 [num_segments, 3]: time, height and width in patches.  Patches lie time by time, and inside it in
+ *              blocks of merge x merge patches, block after block along the width, patch after patch along the width of its
+ *              block (merge = 1: row by row); merge must divide height and width.  Height or width < 1: text.
+ *   first      DEVICE int32 [num_segments], or NULL for zeros: added to all three positions of a segment's tokens
+ *   positions  DEVICE int32 [3, total_tokens] (out): patch (t, y, x) gets first + t, first + y, first + x; token i of a text first + i
+ *              three times; a token in no segment 0
+ * The contents of cu_rows and grids are not validated; whatever they are, nothing outside the tensors is accessed.  1 <= merge <= 64.
+ */
+int varlen_attn_rotary_positions(int32_t total_tokens, int32_t num_segments, int32_t merge, const int32_t *cu_rows,
+                                 const int32_t *grids, const int32_t *first, int32_t *positions, void *hip_stream);
+
+/*
+ * Rotary positions with several axes.  Pair j of a head turns by the angle phi = positions[pair_axis[j]][t] * inv_freq[j]:
+ *     y1 = x1 cos phi - x2 sin phi,    y2 = x2 cos phi + x1 sin phi
+ * where (x1, x2) are channels (j, j + num_pairs), or (2j, 2j + 1) if interleaved.  Channels from 2 num_pairs on are copied, and so
+ * is v if it is given: q, k and v come out of the fused projection as the contiguous tensors that varlen_attn_fwd reads.
+ * varlen_attn_rotary_bwd turns by -phi: q, k, v are then the gradients of the forward's outputs and q_out, k_out, v_out those of its
+ * inputs, which may be parts of the fused projection's gradient.  Angles are formed in 64 bits (any position's is right to
+ * 2^-20), the rotation in fp32, results are rounded to bf16 once.
+ *   q, q_out   bf16 [T, num_q_heads,  head_dim];  k, k_out, v, v_out bf16 [T, num_kv_heads, head_dim]; v and v_out both or neither
+ *   positions  DEVICE int32 [num_axes, total_tokens];  inv_freq  DEVICE fp32 [num_pairs], finite
+ *   pair_axis  DEVICE int32 [num_pairs], each in [0, num_axes); others are taken as the nearest axis
+ * An output may be its own input (same pointer and stride); any other overlap is not allowed.
+ */
+typedef struct {
+    int32_t total_tokens;  /* T >= 0 */
+    int32_t num_q_heads;   /* >= 1 */
+    int32_t num_kv_heads;  /* >= 1 */
+    int32_t head_dim;      /* 2..512 */
+    int32_t num_pairs;     /* 1..head_dim / 2 */
+    int32_t num_axes;      /* 1..8 */
+    int32_t interleaved;   /* 0 or 1 */
+    int64_t q_stride, k_stride, v_stride;             /* each >= heads * head_dim */
+    int64_t q_out_stride, k_out_stride, v_out_stride;
+} varlen_attn_rotary_params;
+int varlen_attn_rotary_fwd(const varlen_attn_rotary_params *p, const void *q, const void *k, const void *v,
+                           const int32_t *positions, const float *inv_freq, const int32_t *pair_axis, void *q_out, void *k_out,
+                           void *v_out, void *hip_stream);
+int varlen_attn_rotary_bwd(const varlen_attn_rotary_params *p, const void *dq, const void *dk, const void *dv,
+                           const int32_t *positions, const float *inv_freq, const int32_t *pair_axis, void *dq_out, void *dk_out,
+                           void *dv_out, void *hip_stream);
+
+/*
+ * Activations in 8 bits.  A row's channels are cut into blocks of VA_ACT8_BLOCK (the last one shorter), each with one fp32
+ *     scale = max(amax * fl(1 / M), 2^-126),   M = 127 (VA_ACT8_INT8) or 448 (VA_ACT8_E4M3, the format's largest number)
+ *     code  = the format's nearest value to x * fl(1 / scale), ties to even;   it stands for code * scale
+ * A value comes back within half a step: amax / 254 in int8, 2^-4 of itself (or 2^-10 scale) in e4m3.  A block with an infinity or
+ * a NaN in it comes back as NaN throughout.  Unpacking rounds code * scale to bf16 once.
+ *   values  bf16: row r of token t starts at t * stride + r * channels, 0 <= r < rows_per_token
+ *   codes   one byte each, [total_tokens, rows_per_token, channels];   scales  fp32 [total_tokens, rows_per_token, blocks]
+ * `tensors` is a HOST array of up to VA_ACT8_MAX_TENSORS, read during the call; all are handled by one launch.
+ */
+enum { VA_ACT8_INT8 = 0, VA_ACT8_E4M3 = 1, VA_ACT8_BLOCK = 128, VA_ACT8_MAX_TENSORS = 8 };
+typedef struct {
+    void *values;            /* pack reads it, unpack writes it */
+    void *codes;             /* pack writes it, unpack reads it, and so the scales */
+    float *scales;
+    int32_t total_tokens;    /* >= 0 */
+    int32_t rows_per_token;  /* >= 1 */
+    int32_t channels;        /* 1..16384 */
+    int64_t stride;          /* of values, >= rows_per_token * channels */
+} varlen_attn_act8_tensor;
+int varlen_attn_act8_pack(const varlen_attn_act8_tensor *tensors, int32_t num_tensors, int32_t format, void *hip_stream);
+int varlen_attn_act8_unpack(const varlen_attn_act8_tensor *tensors, int32_t num_tensors, int32_t format, void *hip_stream);
+
+/*
+ * varlen_attn_bwd from a checkpoint in 8 bits: q, k, v and o as varlen_attn_act8_pack left them (rows of one head, so one scale per
+ * head and token).  The gradients are those of varlen_attn_bwd on the unpacked tensors, with the lse of the forward as it was.
+ * They are unpacked into the workspace, 2 bytes per channel, so the checkpoint saves memory between the two passes, not in this one.
+ */
+size_t varlen_attn_bwd_act8_workspace_bytes(const varlen_attn_params *p);
+int varlen_attn_bwd_act8(const varlen_attn_params *p, int32_t format, const void *dout, const void *q_codes, const float *q_scales,
+                         const void *k_codes, const float *k_scales, const void *v_codes, const float *v_scales,
+                         const void *o_codes, const float *o_scales, const float *lse, const int32_t *cu_seqlens, void *dq,
+                         void *dk, void *dv, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Layer norm of rows of `channels`, one row per token or rows_per_token of them (the heads of q: rows_per_token = Hq, channels = D).
+ *     h = x, or bf16(x + residual), which is then written to `summed`
+ *     mean = sum h / C,   rstd = (sum (h - mean)^2 / C + eps)^(-1/2),   y = (h - mean) rstd weight + bias
+ * weight (and then bias) may be NULL: 1 (and 0).  codes and scales, if given, receive h in 8 bits (act8_format, layout as above) in
+ * the same pass, for the backward.
+ * Backward: with n = (h - mean) rstd and g = dy weight,
+ *     dx = rstd (g - sum g / C - n sum(g n) / C) + dsummed,   dweight = sum over rows of dy n,   dbias = sum over rows of dy
+ * from h in bf16 (x) or in 8 bits (x NULL, codes and scales as the forward left them).  dx is the gradient of x and of residual; dsummed,
+ * the gradient that reaches `summed` on its own way, may be NULL.  dweight and dbias are fp32 and written if weight is given (all
+ * zeros where there are no rows).  Statistics and sums are fp32; the same call gives the same bits.
+ *   x, y, dy, dx, residual, summed, dsummed  bf16;   mean, rstd  fp32 [total_tokens, rows_per_token]
+ *   Only x, dy and dx have strides; the others lie row by row.
+ */
+enum { VA_BF16 = 0, VA_FP32 = 1 };
+typedef struct {
+    int32_t total_tokens;    /* >= 0 */
+    int32_t rows_per_token;  /* >= 1 */
+    int32_t channels;        /* 1..16384 */
+    int32_t weight_type;     /* of weight and bias: VA_BF16 or VA_FP32 */
+    int32_t act8_format;     /* of codes, where there are any */
+    float eps;               /* finite, >= 0 */
+    int64_t x_stride;        /* each >= rows_per_token * channels */
+    int64_t dy_stride;       /* (backward) */
+    int64_t dx_stride;       /* (backward) */
+} varlen_attn_norm_params;
+int varlen_attn_norm_fwd(const varlen_attn_norm_params *p, const void *x, const void *residual, const void *weight,
+                         const void *bias, void *y, void *summed, float *mean, float *rstd, void *codes, float *scales,
+                         void *hip_stream);
+size_t varlen_attn_norm_bwd_workspace_bytes(const varlen_attn_norm_params *p);
+int varlen_attn_norm_bwd(const varlen_attn_norm_params *p, const void *dy, const void *x, const void *codes, const float *scales,
+                         const float *mean, const float *rstd, const void *weight, const void *dsummed, void *dx, float *dweight,
+                         float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Static, NUL-terminated description of a status code. */
 const char *varlen_attn_status_string(int status);
 
@@ -263,7 +387,10 @@ enum {
     VA_KERNEL_DKDV = 2,  /* backward: dK, dV */
     VA_KERNEL_DQ = 3,    /* backward: dQ (also forms Delta = rowsum(dO * O) and writes the per-row statistics
                             dK/dV reads; launched first) */
-    VA_KERNEL_MERGE = 4  /* merge of partial results (varlen_attn_merge, split forward) and sums of a cut backward */
+    VA_KERNEL_MERGE = 4, /* merge of partial results (varlen_attn_merge, split forward) and sums of a cut backward */
+    VA_KERNEL_ROTARY = 5, /* rotary positions and their making */
+    VA_KERNEL_NORM = 6,  /* layer norm, forward and backward */
+    VA_KERNEL_ACT8 = 7   /* packing and unpacking of 8-bit checkpoints */
 };
 int varlen_attn_profile_enable(int on);
 int varlen_attn_profile_read(int kernel, double *total_ms, int64_t *launches);

@@ -1,5 +1,9 @@
 """Python binding of libvarlen_attn.so: argument marshalling only.
 
+Attention: varlen_attn_fwd, varlen_attn_bwd, varlen_attn_merge.  Around it, on the same packed tokens: varlen_attn_rotary_positions,
+varlen_attn_rotary_fwd and _bwd, varlen_attn_norm_fwd and _bwd, varlen_attn_act8_pack and _unpack (activations in 8 bits),
+varlen_attn_bwd_act8 (attention's backward pass from them).
+
 Forward, backward and merge are marshalled in native code (csrc/va_host.cpp) where that is built and nothing is unusual about the
 call, else here.
 Every step of the attention path runs in the library's HIP kernels.  PyTorch is used for device
@@ -13,6 +17,7 @@ import os
 import subprocess
 import threading
 import warnings
+from collections import namedtuple
 
 import torch
 
@@ -37,6 +42,23 @@ class Params(ctypes.Structure):
                 ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32),
                 ("softmax_scale", ctypes.c_float), ("max_seqlen", ctypes.c_int32), ("kv_splits", ctypes.c_int32)]
+
+
+class RotaryParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("total_tokens", "num_q_heads", "num_kv_heads", "head_dim", "num_pairs", "num_axes",
+                                              "interleaved")] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride", "k_out_stride", "v_out_stride")]
+
+
+class Act8Tensor(ctypes.Structure):
+    _fields_ = [("values", ctypes.c_void_p), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("total_tokens", ctypes.c_int32), ("rows_per_token", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("stride", ctypes.c_int64)]
+
+
+class NormParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("total_tokens", "rows_per_token", "channels", "weight_type", "act8_format")] + \
+               [("eps", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("x_stride", "dy_stride", "dx_stride")]
 
 
 def load():
@@ -80,6 +102,17 @@ def load():
     lib.varlen_attn_profile_read.restype = ctypes.c_int
     lib.varlen_attn_profile_clock_probe.argtypes = [vp]
     lib.varlen_attn_profile_clock_probe.restype = ctypes.c_int
+    i32 = ctypes.c_int32
+    rp, ap, np_ = ctypes.POINTER(RotaryParams), ctypes.POINTER(Act8Tensor), ctypes.POINTER(NormParams)
+    for name, args in (("rotary_positions", [i32, i32, i32, vp, vp, vp, vp, vp]), ("rotary_fwd", [rp, *[vp] * 10]),
+                       ("rotary_bwd", [rp, *[vp] * 10]), ("act8_pack", [ap, i32, i32, vp]), ("act8_unpack", [ap, i32, i32, vp]),
+                       ("bwd_act8", [pp, i32, *[vp] * 15, sz, vp]), ("norm_fwd", [np_, *[vp] * 11]),
+                       ("norm_bwd", [np_, *[vp] * 12, sz, vp])):
+        f = getattr(lib, "varlen_attn_" + name)
+        f.argtypes, f.restype = args, ctypes.c_int
+    for name, arg in (("bwd_act8", pp), ("norm_bwd", np_)):
+        f = getattr(lib, f"varlen_attn_{name}_workspace_bytes")
+        f.argtypes, f.restype = [arg], sz
     _lib = lib
     return lib
 
@@ -309,7 +342,7 @@ def varlen_attn_bwd(dout, q, k, v, out, lse, cu_seqlens, causal, softmax_scale, 
     return dq, dk, dv
 
 
-KERNELS = {"sched": 0, "fwd": 1, "dkdv": 2, "dq": 3, "merge": 4}
+KERNELS = {"sched": 0, "fwd": 1, "dkdv": 2, "dq": 3, "merge": 4, "rotary": 5, "norm": 6, "act8": 7}
 
 
 def profile_enable(on=True):
@@ -357,6 +390,342 @@ def varlen_attn_merge(o_parts, lse_parts, out=None, lse=None, stream=None):
     _check(load().varlen_attn_merge(ctypes.byref(p), P, o_parts.data_ptr(), lse_parts.data_ptr(), out.data_ptr(),
                                     lse.data_ptr(), _stream_handle(stream)))
     return out, lse
+
+
+# ---- around attention: rotary positions, layer norm, activations in 8 bits --------------------------------------------------
+
+Act8 = namedtuple("Act8", ["codes", "scales"])
+Act8.__doc__ = """A tensor in 8 bits: codes (torch.int8 or torch.float8_e4m3fn, the tensor's shape) and their fp32 scales, one for each
+ACT8_BLOCK channels of a row (the shape without the last dimension, and the number of blocks)."""
+NormForward = namedtuple("NormForward", ["out", "mean", "rstd", "summed", "saved"])
+
+ACT8_BLOCK = 128
+_ACT8_FORMATS = {"int8": (0, torch.int8), "e4m3": (1, torch.float8_e4m3fn)}
+_ACT8_OF_TYPE = {torch.int8: 0, torch.float8_e4m3fn: 1}
+_WEIGHT_TYPES = {torch.bfloat16: 0, torch.float32: 1}
+
+
+class _On:
+    """Everything a call is given has to be on one GPU, which is made the current one for it."""
+
+    def __init__(self, first, stream, /, **tensors):
+        for name, t in tensors.items():
+            if t is not None and t.device != first.device:
+                raise ValueError(f"{name} must be on {first.device}")
+        self._guard = torch.cuda.device(first.device)
+        self._stream, self._device = stream, first.device
+
+    def __enter__(self):
+        self._guard.__enter__()
+        s = torch.cuda.current_stream(self._device) if self._stream is None else self._stream
+        self.stream = ctypes.c_void_p(s.cuda_stream)
+        self._alloc = _Allocating(self._stream, self._device)
+        self._alloc.__enter__()
+        return self
+
+    def __exit__(self, *error):
+        self._alloc.__exit__(*error)
+        self._guard.__exit__(*error)
+
+    def empty(self, shape, dtype):
+        return self._alloc.result(torch.empty(shape, dtype=dtype, device=self._device))
+
+    def scratch(self, n):
+        return torch.empty(max(n, 16), dtype=torch.uint8, device=self._device)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _token_stride(t, name, dims=(3,)):
+    """Elements from one token to the next of a bf16 tensor [T, H, D] (or [T, C]) on the GPU, whose channels (and heads) lie side by
+    side: contiguous, or a part of a wider tensor."""
+    if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() in dims):
+        raise ValueError(f"{name} must be a torch.bfloat16 tensor of {' or '.join(map(str, dims))} dimensions on the GPU")
+    shape, strides = t.shape, t.stride()
+    width = shape[1] if t.dim() == 2 else shape[1] * shape[2]
+    if t.numel() == 0:
+        return width
+    if (shape[-1] > 1 and strides[-1] != 1) or (t.dim() == 3 and shape[1] > 1 and strides[1] != shape[2]) or \
+            (shape[0] > 1 and strides[0] < width):
+        raise ValueError(f"{name} must hold a token's channels side by side")
+    return strides[0] if shape[0] > 1 else width
+
+
+def _out_like(t, shape, name):
+    """A caller's own output tensor: of this shape."""
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape)}")
+
+
+def varlen_attn_rotary_positions(cu_rows, grids, total_tokens, first=None, merge=1, out=None, stream=None):
+    """Positions int32 [3, total_tokens] (time, height, width) of packed text, images and video; asynchronous on the stream.
+    Segment s holds the tokens [cu_rows[s], cu_rows[s + 1]); grids int32 [S, 3] its time, height and width in patches, laid out in blocks of
+    merge x merge (height or width 0: text, whose tokens count up on all axes); first int32 [S]: added to a segment's positions."""
+    for t, n in ((cu_rows, "cu_rows"), (grids, "grids"), (first, "first"), (out, "out")):
+        if t is not None:
+            _require(t, torch.int32, n)
+    segments = cu_rows.numel() - 1
+    if cu_rows.dim() != 1 or segments < 0 or tuple(grids.shape) != (segments, 3):
+        raise ValueError("grids must be [S, 3] for the S + 1 elements of cu_rows")
+    if first is not None and first.numel() != segments:
+        raise ValueError("first must be [S]")
+    _out_like(out, (3, int(total_tokens)), "out")
+    with _On(cu_rows, stream, grids=grids, first=first, out=out) as on:
+        out = on.empty((3, int(total_tokens)), torch.int32) if out is None else out
+        _check(load().varlen_attn_rotary_positions(int(total_tokens), segments, int(merge), cu_rows.data_ptr(), grids.data_ptr(),
+                                                   _ptr(first), out.data_ptr(), on.stream))
+    return out
+
+
+def _rotary(inverse, names, q, k, v, positions, inv_freq, pair_axis, interleaved, q_out, k_out, v_out, stream):
+    ins, outs = dict(zip(names, (q, k, v))), dict(zip((n + "_out" for n in names), (q_out, k_out, v_out)))
+    strides = [0 if t is None else _token_stride(t, n) for n, t in ins.items()]
+    if k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+        raise ValueError(f"{names[1]} must be [T, Hkv, D] matching {names[0]}'s T and D")
+    if v is not None and v.shape != k.shape:
+        raise ValueError(f"{names[2]} must match {names[1]}")
+    if v is None and v_out is not None:
+        raise ValueError(f"{names[2]} must be given with {names[2]}_out")
+    _require(positions, torch.int32, "positions")
+    _require(inv_freq, torch.float32, "inv_freq")
+    _require(pair_axis, torch.int32, "pair_axis")
+    if positions.dim() != 2 or positions.shape[1] != q.shape[0]:
+        raise ValueError("positions must be [axes, T]")
+    if inv_freq.dim() != 1 or pair_axis.shape != inv_freq.shape:
+        raise ValueError("pair_axis must match inv_freq")
+    for (n, t), like in zip(outs.items(), (q, k, v)):
+        if t is not None:
+            _out_like(t, like.shape, n)
+    out_strides = [0 if like is None else _token_stride(t, n) if t is not None else like.shape[1] * like.shape[2]
+                   for (n, t), like in zip(outs.items(), (q, k, v))]
+    p = RotaryParams(q.shape[0], q.shape[1], k.shape[1], q.shape[2], inv_freq.numel(), positions.shape[0], int(bool(interleaved)),
+                     *strides, *out_strides)
+    with _On(q, stream, **ins, **outs, positions=positions, inv_freq=inv_freq, pair_axis=pair_axis) as on:
+        made = [like if like is None else on.empty(like.shape, torch.bfloat16) if t is None else t
+                for t, like in zip((q_out, k_out, v_out), (q, k, v))]
+        f = load().varlen_attn_rotary_bwd if inverse else load().varlen_attn_rotary_fwd
+        _check(f(ctypes.byref(p), q.data_ptr(), k.data_ptr(), _ptr(v), positions.data_ptr(), inv_freq.data_ptr(),
+                 pair_axis.data_ptr(), *map(_ptr, made), on.stream))
+    return tuple(made[:2] if v is None else made)
+
+
+def varlen_attn_rotary_fwd(q, k, positions, inv_freq, pair_axis, v=None, interleaved=False, q_out=None, k_out=None, v_out=None,
+                           stream=None):
+    """q and k turned by their tokens' positions, as (q, k), or (q, k, v) with v copied along; asynchronous on the stream.
+    q [T, Hq, D], k and v [T, Hkv, D]: bf16, contiguous or parts of the fused projection [T, Hq + 2 Hkv, D].
+    positions int32 [axes, T]; inv_freq fp32 [P] and pair_axis int32 [P]: frequency and axis of each pair of channels, (j, j + P), or
+    (2j, 2j + 1) if interleaved; channels from 2P on are copied.
+    q_out, k_out, v_out: the caller's own tensors of the same shapes, contiguous or parts too; each may be its own input."""
+    return _rotary(False, ("q", "k", "v"), q, k, v, positions, inv_freq, pair_axis, interleaved, q_out, k_out, v_out, stream)
+
+
+def varlen_attn_rotary_bwd(dq, dk, positions, inv_freq, pair_axis, dv=None, interleaved=False, dq_out=None, dk_out=None, dv_out=None,
+                           stream=None):
+    """The gradients of varlen_attn_rotary_fwd's inputs from those of its outputs; arguments as there."""
+    return _rotary(True, ("dq", "dk", "dv"), dq, dk, dv, positions, inv_freq, pair_axis, interleaved, dq_out, dk_out, dv_out, stream)
+
+
+def _act8_shape(shape):
+    return (*shape[:-1], (shape[-1] + ACT8_BLOCK - 1) // ACT8_BLOCK)
+
+
+def _check_act8(x, name):
+    """Format, tokens, rows a token and channels of an Act8."""
+    if not isinstance(x, Act8):
+        raise ValueError(f"{name} must be an Act8 (codes, scales)")
+    codes, scales = x
+    if not (codes.is_cuda and codes.dtype in _ACT8_OF_TYPE and codes.is_contiguous() and codes.dim() in (2, 3)):
+        raise ValueError(f"{name}.codes must be a contiguous torch.int8 or torch.float8_e4m3fn tensor of 2 or 3 dimensions on the GPU")
+    _require(scales, torch.float32, f"{name}.scales")
+    if tuple(scales.shape) != _act8_shape(codes.shape) or scales.device != codes.device:
+        raise ValueError(f"{name}.scales must be {_act8_shape(codes.shape)} on {codes.device}")
+    return _ACT8_OF_TYPE[codes.dtype]
+
+
+def _act8_tensor(values, stride, codes, scales):
+    shape = codes.shape
+    return Act8Tensor(values.data_ptr(), codes.data_ptr(), scales.data_ptr(), shape[0], 1 if len(shape) == 2 else shape[1], shape[-1],
+                      stride)
+
+
+def varlen_attn_act8_pack(tensors, format="int8", out=None, stream=None):
+    """bf16 tensors [T, C] or [T, H, C] (contiguous or parts of wider ones) in 8 bits, a list of Act8; asynchronous on the stream.
+    format: "int8" or "e4m3".  One launch for up to 8 tensors.  out: Act8s of the caller's own."""
+    if format not in _ACT8_FORMATS:
+        raise ValueError("format must be int8 or e4m3")
+    number, code_type = _ACT8_FORMATS[format]
+    tensors = list(tensors)
+    strides = [_token_stride(t, f"tensors[{i}]", (2, 3)) for i, t in enumerate(tensors)]
+    if out is not None:
+        out = list(out)
+        if len(out) != len(tensors):
+            raise ValueError("out must match tensors")
+        for i, (t, o) in enumerate(zip(tensors, out)):
+            if _check_act8(o, f"out[{i}]") != number or o.codes.shape != t.shape:
+                raise ValueError(f"out[{i}] must match tensors[{i}] and the format")
+    if not tensors:
+        return []
+    given = {} if out is None else {f"out[{i}]": o.codes for i, o in enumerate(out)}
+    with _On(tensors[0], stream, **{f"tensors[{i}]": t for i, t in enumerate(tensors)}, **given) as on:
+        if out is None:
+            out = [Act8(on.empty(t.shape, code_type), on.empty(_act8_shape(t.shape), torch.float32)) for t in tensors]
+        for at in range(0, len(tensors), 8):
+            part = [_act8_tensor(t, s, *o) for t, s, o in zip(tensors[at:at + 8], strides[at:at + 8], out[at:at + 8])]
+            _check(load().varlen_attn_act8_pack((Act8Tensor * len(part))(*part), len(part), number, on.stream))
+    return out
+
+
+def varlen_attn_act8_unpack(packed, out=None, stream=None):
+    """The bf16 tensors that a list of Act8 stands for; asynchronous on the stream.
+    out: the caller's own tensors of the same shapes, contiguous or parts of wider ones."""
+    packed = list(packed)
+    formats = [_check_act8(x, f"packed[{i}]") for i, x in enumerate(packed)]
+    if len(set(formats)) > 1:
+        raise ValueError("packed must be of one format")
+    if out is not None:
+        out = list(out)
+        if len(out) != len(packed):
+            raise ValueError("out must match packed")
+        for i, (x, o) in enumerate(zip(packed, out)):
+            _out_like(o, x.codes.shape, f"out[{i}]")
+    if not packed:
+        return []
+    strides = [x.codes[0].numel() if x.codes.shape[0] else 1 << 30 for x in packed] if out is None else \
+        [_token_stride(o, f"out[{i}]", (2, 3)) for i, o in enumerate(out)]
+    given = {} if out is None else {f"out[{i}]": o for i, o in enumerate(out)}
+    with _On(packed[0].codes, stream, **{f"packed[{i}]": x.codes for i, x in enumerate(packed)}, **given) as on:
+        if out is None:
+            out = [on.empty(x.codes.shape, torch.bfloat16) for x in packed]
+        for at in range(0, len(packed), 8):
+            part = [_act8_tensor(o, s, *x) for x, s, o in zip(packed[at:at + 8], strides[at:at + 8], out[at:at + 8])]
+            _check(load().varlen_attn_act8_unpack((Act8Tensor * len(part))(*part), len(part), formats[0], on.stream))
+    return out
+
+
+def bwd_act8_workspace_bytes(params):
+    return int(load().varlen_attn_bwd_act8_workspace_bytes(ctypes.byref(params)))
+
+
+def varlen_attn_bwd_act8(dout, q, k, v, out, lse, cu_seqlens, causal, softmax_scale, dq=None, dk=None, dv=None, workspace=None,
+                         stream=None, max_seqlen=0, kv_splits=0):
+    """varlen_attn_bwd with q, k, v and out in 8 bits (Act8s of one format, from varlen_attn_act8_pack); the other arguments as there."""
+    _require(dout, torch.bfloat16, "dout")
+    formats = {_check_act8(x, n) for x, n in ((q, "q"), (k, "k"), (v, "v"), (out, "out"))}
+    if len(formats) > 1:
+        raise ValueError("q, k, v and out must be of one format")
+    _require(lse, torch.float32, "lse")
+    _require(cu_seqlens, torch.int32, "cu_seqlens")
+    qs, ks = q.codes.shape, k.codes.shape
+    if dout.dim() != 3 or dout.shape != qs or out.codes.shape != qs:
+        raise ValueError("dout and out must match q")
+    if len(ks) != 3 or v.codes.shape != ks or ks[0] != qs[0] or ks[2] != qs[2]:
+        raise ValueError("k and v must be [T, Hkv, D] matching q's T and D")
+    _require_room(lse, torch.float32, "lse", qs[0] * qs[1])
+    for t, shape, n in ((dq, qs, "dq"), (dk, ks, "dk"), (dv, ks, "dv")):
+        _require_room(t, torch.bfloat16, n, shape.numel())
+    _require_room(workspace, None, "workspace")
+    p = _params_of(q.codes, k.codes, cu_seqlens, causal, softmax_scale, kv_splits, max_seqlen)
+    with _On(dout, stream, q=q.codes, k=k.codes, v=v.codes, out=out.codes, lse=lse, cu_seqlens=cu_seqlens) as on:
+        dq = on.empty(qs, torch.bfloat16) if dq is None else dq
+        dk = on.empty(ks, torch.bfloat16) if dk is None else dk
+        dv = on.empty(ks, torch.bfloat16) if dv is None else dv
+        if workspace is None:
+            workspace = on.scratch(bwd_act8_workspace_bytes(p))
+        _check(load().varlen_attn_bwd_act8(ctypes.byref(p), formats.pop(), dout.data_ptr(),
+                                           *(t.data_ptr() for x in (q, k, v, out) for t in x), lse.data_ptr(), cu_seqlens.data_ptr(),
+                                           dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                           on.stream))
+    return dq, dk, dv
+
+
+def _check_weights(weight, bias, channels):
+    if bias is not None and weight is None:
+        raise ValueError("weight must be given with bias")
+    for t, n in ((weight, "weight"), (bias, "bias")):
+        if t is None:
+            continue
+        if not (t.is_cuda and t.dtype in _WEIGHT_TYPES and t.is_contiguous() and tuple(t.shape) == (channels,)):
+            raise ValueError(f"{n} must be a contiguous torch.bfloat16 or torch.float32 tensor [{channels}] on the GPU")
+    if bias is not None and bias.dtype != weight.dtype:
+        raise ValueError("bias must have weight's type")
+    return 0 if weight is None else _WEIGHT_TYPES[weight.dtype]
+
+
+def _contiguous_like(t, shape, name):
+    if t is not None:
+        _require(t, torch.bfloat16, name)
+        _out_like(t, shape, name)
+
+
+def _norm_params(shape, weight_type, act8_format, eps, x_stride=0, dy_stride=0, dx_stride=0):
+    return NormParams(shape[0], 1 if len(shape) == 2 else shape[1], shape[-1], weight_type, act8_format, float(eps), x_stride, dy_stride,
+                      dx_stride)
+
+
+def varlen_attn_norm_fwd(x, weight=None, bias=None, eps=1e-5, residual=None, save=None, out=None, stream=None):
+    """Layer norm over the last dimension of x, bf16 [T, C] or [T, H, C] (contiguous or a part of a wider tensor): a NormForward
+    (out bf16, mean and rstd fp32 [T] or [T, H], summed, saved); asynchronous on the stream.
+    weight, bias: bf16 or fp32 [C], or None.  residual: contiguous, x's shape; the norm is then of summed = bf16(x + residual).
+    save: "int8" or "e4m3": what is normed is left in 8 bits too (saved, an Act8), for varlen_attn_norm_bwd.
+    out: the caller's own contiguous tensor of x's shape."""
+    stride = _token_stride(x, "x", (2, 3))
+    shape = x.shape
+    if save is not None and save not in _ACT8_FORMATS:
+        raise ValueError("save must be int8 or e4m3")
+    number, code_type = _ACT8_FORMATS[save or "int8"]
+    _contiguous_like(residual, shape, "residual")
+    _contiguous_like(out, shape, "out")
+    p = _norm_params(shape, _check_weights(weight, bias, shape[-1]), number, eps, x_stride=stride)
+    with _On(x, stream, weight=weight, bias=bias, residual=residual, out=out) as on:
+        out = on.empty(shape, torch.bfloat16) if out is None else out
+        mean, rstd = on.empty(shape[:-1], torch.float32), on.empty(shape[:-1], torch.float32)
+        summed = None if residual is None else on.empty(shape, torch.bfloat16)
+        saved = None if save is None else Act8(on.empty(shape, code_type), on.empty(_act8_shape(shape), torch.float32))
+        codes, scales = saved or (None, None)
+        _check(load().varlen_attn_norm_fwd(ctypes.byref(p), x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), out.data_ptr(),
+                                           _ptr(summed), mean.data_ptr(), rstd.data_ptr(), _ptr(codes), _ptr(scales), on.stream))
+    return NormForward(out, mean, rstd, summed, saved)
+
+
+def norm_bwd_workspace_bytes(params):
+    return int(load().varlen_attn_norm_bwd_workspace_bytes(ctypes.byref(params)))
+
+
+def varlen_attn_norm_bwd(dy, x, mean, rstd, weight=None, dsummed=None, dx=None, workspace=None, stream=None):
+    """(dx bf16, dweight fp32, dbias fp32; the last two None without weight) of varlen_attn_norm_fwd; asynchronous on the stream.
+    x: what was normed: the forward's x, its summed where it had a residual, or its saved Act8.  mean, rstd: the forward's.
+    dsummed: the gradient that reaches summed on its own way, added to dx (which is the gradient of x and of residual).
+    dy, x and dx may be parts of wider tensors; dx, workspace: the caller's own."""
+    dy_stride = _token_stride(dy, "dy", (2, 3))
+    shape, packed = dy.shape, isinstance(x, Act8)
+    number = _check_act8(x, "x") if packed else 0
+    x_stride = 0 if packed else _token_stride(x, "x", (2, 3))
+    if (x.codes if packed else x).shape != shape:
+        raise ValueError("x must match dy")
+    for t, n in ((mean, "mean"), (rstd, "rstd")):
+        _require(t, torch.float32, n)
+        _out_like(t, shape[:-1], n)
+    _contiguous_like(dsummed, shape, "dsummed")
+    dx_stride = shape[1:].numel()
+    if dx is not None:
+        dx_stride = _token_stride(dx, "dx", (2, 3))
+        _out_like(dx, shape, "dx")
+    _require_room(workspace, None, "workspace")
+    p = _norm_params(shape, _check_weights(weight, None, shape[-1]), number, 0.0, x_stride, dy_stride, dx_stride)
+    codes, scales = x if packed else (None, None)
+    with _On(dy, stream, x=x.codes if packed else x, mean=mean, rstd=rstd, weight=weight, dsummed=dsummed, dx=dx) as on:
+        dx = on.empty(shape, torch.bfloat16) if dx is None else dx
+        dweight = dbias = None
+        if weight is not None:
+            dweight, dbias = on.empty(shape[-1:], torch.float32), on.empty(shape[-1:], torch.float32)
+            if workspace is None:
+                workspace = on.scratch(norm_bwd_workspace_bytes(p))
+        _check(load().varlen_attn_norm_bwd(ctypes.byref(p), dy.data_ptr(), None if packed else x.data_ptr(), _ptr(codes), _ptr(scales),
+                                           mean.data_ptr(), rstd.data_ptr(), _ptr(weight), _ptr(dsummed), dx.data_ptr(), _ptr(dweight),
+                                           _ptr(dbias), _ptr(workspace), 0 if workspace is None else workspace.numel(), on.stream))
+    return dx, dweight, dbias
 
 
 def check_cu_seqlens(cu_seqlens, total_tokens, stream=None):

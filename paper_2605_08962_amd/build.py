@@ -31,7 +31,10 @@ SOURCES = [("va_api.hip", "va_api.o", []), ("va_sched.hip", "va_sched.o", []), (
            ("va_bwd.hip", "va_bwd_dq.o", ["-DVA_BWD_PART=2", "-mllvm", _SCHED + "iterative-ilp"]),
            ("va_bwd.hip", "va_bwd_dkdv80.o", ["-DVA_BWD_PART=3", "-mllvm", _SCHED + "iterative-minreg"]),
            ("va_bwd.hip", "va_bwd_dkdv128.o", ["-DVA_BWD_PART=4", "-mllvm", _SCHED + "iterative-maxocc", *_VGPR_FORM]),
-           ("va_partition.hip", "va_partition.o", []), ("va_merge.hip", "va_merge.o", [])]
+           ("va_partition.hip", "va_partition.o", []), ("va_merge.hip", "va_merge.o", []),
+           # (these keep NaN: an input's comes out as NaN)
+           ("va_rotary.hip", "va_rotary.o", ["-fhonor-nans"]), ("va_norm.hip", "va_norm.o", ["-fhonor-nans"]),
+           ("va_act8.hip", "va_act8.o", ["-fhonor-nans"])]
 # -packed-fp32-ops is switched off on purpose: hipcc must not form v_pk_*_f32 from float code.
 # -fno-honor-nans: the kernels never produce NaN from finite inputs (masked scores use a finite
 # sentinel), and without it every fmaxf of an MFMA result costs an extra canonicalising v_max.

@@ -2,12 +2,15 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
 #include "../../include/varlen_attn.h"
 #include "va_internal.h"
 #include "va_small.h"
+
+static_assert(va::ACT8_MAX_TENSORS == VA_ACT8_MAX_TENSORS, "tensors of one launch");
 
 // Scratch of varlen_attn_fwd_static_scratch: device memory that belongs to the library's code object, one
 // copy per GPU.  In host code this name is only a handle for hipGetSymbolAddress, never an address.
@@ -535,6 +538,254 @@ int varlen_attn_bwd(const varlen_attn_params* p, const void* dout, const void* q
         if (e != hipSuccess) return hip_fail(e);
     }
     return VA_OK;
+}
+
+// ---- operators around attention -------------------------------------------------------------------------------------------
+}  // extern "C"
+namespace {
+
+bool aligned_to(size_t n, std::initializer_list<const void*> ptrs) {
+    for (const void* p : ptrs)
+        if ((uintptr_t)p % n) return false;
+    return true;
+}
+bool any_null(std::initializer_list<const void*> ptrs) {
+    for (const void* p : ptrs)
+        if (!p) return true;
+    return false;
+}
+
+int rotary_impl(const varlen_attn_rotary_params* p, const void* q, const void* k, const void* v, const int32_t* positions,
+                const float* inv_freq, const int32_t* pair_axis, void* q_out, void* k_out, void* v_out, bool inverse, void* hip_stream) {
+    if (!p) return VA_ERR_NULL_PTR;
+    if (p->total_tokens < 0 || p->num_q_heads < 1 || p->num_kv_heads < 1 || p->num_pairs < 1 || p->num_axes < 1 ||
+        p->num_axes > 8 || (p->interleaved != 0 && p->interleaved != 1))
+        return VA_ERR_BAD_SHAPE;
+    if (p->head_dim < 2 || p->head_dim > 512) return VA_ERR_UNSUPPORTED;
+    const int64_t qw = (int64_t)p->num_q_heads * p->head_dim, kw = (int64_t)p->num_kv_heads * p->head_dim;
+    // (a token's items are counted in 32 bits, eight tokens at a time)
+    if (2 * p->num_pairs > p->head_dim || qw + 2 * kw > INT32_MAX / 16 || p->q_stride < qw || p->q_out_stride < qw ||
+        p->k_stride < kw || p->k_out_stride < kw || ((v || v_out) && (p->v_stride < kw || p->v_out_stride < kw)))
+        return VA_ERR_BAD_SHAPE;
+    if (p->total_tokens == 0) return VA_OK;
+    if (any_null({q, k, positions, inv_freq, pair_axis, q_out, k_out}) || !v != !v_out) return VA_ERR_NULL_PTR;
+    if (!aligned_to(2, {q, k, v, q_out, k_out, v_out}) || !aligned_to(4, {positions, inv_freq, pair_axis})) return VA_ERR_MISALIGNED;
+    const int rc = check_device();
+    if (rc != VA_OK) return rc;
+    va::RotaryArgs a{};
+    a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v;
+    a.q_out = (uint16_t*)q_out; a.k_out = (uint16_t*)k_out; a.v_out = (uint16_t*)v_out;
+    a.q_stride = p->q_stride; a.k_stride = p->k_stride; a.v_stride = p->v_stride;
+    a.q_out_stride = p->q_out_stride; a.k_out_stride = p->k_out_stride; a.v_out_stride = p->v_out_stride;
+    a.positions = positions; a.inv_freq = inv_freq; a.pair_axis = pair_axis;
+    a.total_tokens = p->total_tokens; a.num_q_heads = p->num_q_heads; a.num_kv_heads = p->num_kv_heads;
+    a.head_dim = p->head_dim; a.num_pairs = p->num_pairs; a.num_axes = p->num_axes;
+    a.interleaved = p->interleaved; a.inverse = inverse;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    ProfScope ps(VA_KERNEL_ROTARY, stream);
+    const hipError_t e = va::launch_rotary(a, stream);
+    return e == hipSuccess ? VA_OK : hip_fail(e);
+}
+
+int act8_args(const varlen_attn_act8_tensor* t, int32_t num, int32_t format, va::Act8Args& a) {
+    if (num < 0 || num > VA_ACT8_MAX_TENSORS || (format != VA_ACT8_INT8 && format != VA_ACT8_E4M3)) return VA_ERR_BAD_SHAPE;
+    if (num > 0 && !t) return VA_ERR_NULL_PTR;
+    int64_t wgs = 0;
+    a = va::Act8Args{};
+    a.format = format;
+    for (int i = 0; i < num; ++i) {
+        const varlen_attn_act8_tensor& x = t[i];
+        if (x.total_tokens < 0 || x.rows_per_token < 1 || x.channels < 1 || x.stride < (int64_t)x.rows_per_token * x.channels)
+            return VA_ERR_BAD_SHAPE;
+        if (x.channels > 16384) return VA_ERR_UNSUPPORTED;
+        if (x.total_tokens == 0) continue;
+        if (any_null({x.values, x.codes, x.scales})) return VA_ERR_NULL_PTR;
+        if (!aligned_to(2, {x.values}) || !aligned_to(4, {x.scales})) return VA_ERR_MISALIGNED;
+        const int64_t rows = (int64_t)x.total_tokens * x.rows_per_token, blocks = (x.channels + VA_ACT8_BLOCK - 1) / VA_ACT8_BLOCK;
+        if (rows > (int64_t)1 << 40) return VA_ERR_BAD_SHAPE;
+        wgs += rows * blocks / 16 + 1;  // (the launch is one-dimensional)
+        if (wgs > INT32_MAX) return VA_ERR_BAD_SHAPE;
+        a.t[a.num++] = va::Act8Tensor{x.values, x.codes, x.scales, rows, x.stride, x.rows_per_token, x.channels, 0};
+    }
+    return VA_OK;
+}
+
+int act8_impl(const varlen_attn_act8_tensor* t, int32_t num, int32_t format, bool pack, void* hip_stream) {
+    va::Act8Args a;
+    int rc = act8_args(t, num, format, a);
+    if (rc != VA_OK || a.num == 0) return rc;
+    rc = check_device();
+    if (rc != VA_OK) return rc;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    ProfScope ps(VA_KERNEL_ACT8, stream);
+    const hipError_t e = pack ? va::launch_act8_pack(a, stream) : va::launch_act8_unpack(a, stream);
+    return e == hipSuccess ? VA_OK : hip_fail(e);
+}
+
+// Where varlen_attn_bwd_act8 unpacks to, in front of the backward's own workspace.
+struct Act8Layout {
+    size_t q, k, v, o, end;
+};
+Act8Layout act8_layout(const varlen_attn_params* p) {
+    auto bytes = [&](int heads) { return ((size_t)p->total_tokens * heads * p->head_dim * 2 + 255) / 256 * 256; };
+    Act8Layout l;
+    l.q = 0;
+    l.k = l.q + bytes(p->num_q_heads);
+    l.v = l.k + bytes(p->num_kv_heads);
+    l.o = l.v + bytes(p->num_kv_heads);
+    l.end = l.o + bytes(p->num_q_heads);
+    return l;
+}
+
+int check_norm(const varlen_attn_norm_params* p) {
+    if (!p) return VA_ERR_NULL_PTR;
+    if (p->total_tokens < 0 || p->rows_per_token < 1 || p->channels < 1 || (p->weight_type != VA_BF16 && p->weight_type != VA_FP32) ||
+        (p->act8_format != VA_ACT8_INT8 && p->act8_format != VA_ACT8_E4M3))
+        return VA_ERR_BAD_SHAPE;
+    if (p->channels > 16384) return VA_ERR_UNSUPPORTED;
+    if (!std::isfinite(p->eps) || p->eps < 0.f) return VA_ERR_BAD_SCALE;
+    if ((int64_t)p->total_tokens * p->rows_per_token > (int64_t)1 << 40) return VA_ERR_BAD_SHAPE;
+    return VA_OK;
+}
+va::NormArgs norm_args(const varlen_attn_norm_params* p) {
+    va::NormArgs a{};
+    a.rows = (int64_t)p->total_tokens * p->rows_per_token;
+    a.rows_per_token = p->rows_per_token;
+    a.channels = p->channels;
+    a.weight_type = p->weight_type;
+    a.format = -1;
+    a.eps = p->eps;
+    return a;
+}
+
+}  // namespace
+extern "C" {
+
+int varlen_attn_rotary_positions(int32_t total_tokens, int32_t num_segments, int32_t merge, const int32_t* cu_rows,
+                                 const int32_t* grids, const int32_t* first, int32_t* positions, void* hip_stream) {
+    if (total_tokens < 0 || num_segments < 0 || merge < 1 || merge > 64) return VA_ERR_BAD_SHAPE;
+    if (total_tokens == 0) return VA_OK;
+    if (!positions || (num_segments > 0 && any_null({cu_rows, grids}))) return VA_ERR_NULL_PTR;
+    if (!aligned_to(4, {cu_rows, grids, first, positions})) return VA_ERR_MISALIGNED;
+    const int rc = check_device();
+    if (rc != VA_OK) return rc;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    ProfScope ps(VA_KERNEL_ROTARY, stream);
+    const hipError_t e = va::launch_rotary_positions(total_tokens, num_segments, merge, cu_rows, grids, first, positions, stream);
+    return e == hipSuccess ? VA_OK : hip_fail(e);
+}
+
+int varlen_attn_rotary_fwd(const varlen_attn_rotary_params* p, const void* q, const void* k, const void* v,
+                           const int32_t* positions, const float* inv_freq, const int32_t* pair_axis, void* q_out, void* k_out,
+                           void* v_out, void* hip_stream) {
+    return rotary_impl(p, q, k, v, positions, inv_freq, pair_axis, q_out, k_out, v_out, false, hip_stream);
+}
+
+int varlen_attn_rotary_bwd(const varlen_attn_rotary_params* p, const void* dq, const void* dk, const void* dv,
+                           const int32_t* positions, const float* inv_freq, const int32_t* pair_axis, void* dq_out, void* dk_out,
+                           void* dv_out, void* hip_stream) {
+    return rotary_impl(p, dq, dk, dv, positions, inv_freq, pair_axis, dq_out, dk_out, dv_out, true, hip_stream);
+}
+
+int varlen_attn_act8_pack(const varlen_attn_act8_tensor* tensors, int32_t num_tensors, int32_t format, void* hip_stream) {
+    return act8_impl(tensors, num_tensors, format, true, hip_stream);
+}
+
+int varlen_attn_act8_unpack(const varlen_attn_act8_tensor* tensors, int32_t num_tensors, int32_t format, void* hip_stream) {
+    return act8_impl(tensors, num_tensors, format, false, hip_stream);
+}
+
+size_t varlen_attn_bwd_act8_workspace_bytes(const varlen_attn_params* p) {
+    if (check_params(p) != VA_OK) return 0;
+    return act8_layout(p).end + bwd_layout(p).end;
+}
+
+int varlen_attn_bwd_act8(const varlen_attn_params* p, int32_t format, const void* dout, const void* q_codes, const float* q_scales,
+                         const void* k_codes, const float* k_scales, const void* v_codes, const float* v_scales,
+                         const void* o_codes, const float* o_scales, const float* lse, const int32_t* cu_seqlens, void* dq,
+                         void* dk, void* dv, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = check_params(p);
+    if (rc != VA_OK) return rc;
+    if (format != VA_ACT8_INT8 && format != VA_ACT8_E4M3) return VA_ERR_BAD_SHAPE;
+    if (p->total_tokens == 0 || p->num_seqs == 0) return VA_OK;
+    if (any_null({dout, q_codes, q_scales, k_codes, k_scales, v_codes, v_scales, o_codes, o_scales, lse, cu_seqlens, dq, dk, dv, workspace}))
+        return VA_ERR_NULL_PTR;
+    if (!aligned_to(16, {dout, dq, dk, dv, workspace}) || !aligned_to(4, {q_scales, k_scales, v_scales, o_scales, lse, cu_seqlens}))
+        return VA_ERR_MISALIGNED;
+    const Act8Layout l = act8_layout(p);
+    if (workspace_bytes < l.end || workspace_bytes - l.end < bwd_layout(p, workspace_bytes - l.end).end) return VA_ERR_WORKSPACE_TOO_SMALL;
+    char* const ws = (char*)workspace;
+    const int32_t T = p->total_tokens, D = p->head_dim, Hq = p->num_q_heads, Hkv = p->num_kv_heads;
+    const varlen_attn_act8_tensor kept[4] = {
+        {ws + l.q, const_cast<void*>(q_codes), const_cast<float*>(q_scales), T, Hq, D, (int64_t)Hq * D},
+        {ws + l.k, const_cast<void*>(k_codes), const_cast<float*>(k_scales), T, Hkv, D, (int64_t)Hkv * D},
+        {ws + l.v, const_cast<void*>(v_codes), const_cast<float*>(v_scales), T, Hkv, D, (int64_t)Hkv * D},
+        {ws + l.o, const_cast<void*>(o_codes), const_cast<float*>(o_scales), T, Hq, D, (int64_t)Hq * D}};
+    rc = act8_impl(kept, 4, format, false, hip_stream);
+    if (rc != VA_OK) return rc;
+    return varlen_attn_bwd(p, dout, ws + l.q, ws + l.k, ws + l.v, ws + l.o, lse, cu_seqlens, dq, dk, dv, ws + l.end,
+                           workspace_bytes - l.end, hip_stream);
+}
+
+int varlen_attn_norm_fwd(const varlen_attn_norm_params* p, const void* x, const void* residual, const void* weight,
+                         const void* bias, void* y, void* summed, float* mean, float* rstd, void* codes, float* scales,
+                         void* hip_stream) {
+    int rc = check_norm(p);
+    if (rc != VA_OK) return rc;
+    if (p->x_stride < (int64_t)p->rows_per_token * p->channels) return VA_ERR_BAD_SHAPE;
+    if (p->total_tokens == 0) return VA_OK;
+    if (any_null({x, y, mean, rstd}) || !residual != !summed || !codes != !scales || (bias && !weight)) return VA_ERR_NULL_PTR;
+    const size_t wa = p->weight_type == VA_BF16 ? 2 : 4;
+    if (!aligned_to(2, {x, residual, y, summed}) || !aligned_to(4, {mean, rstd, scales}) || !aligned_to(wa, {weight, bias}))
+        return VA_ERR_MISALIGNED;
+    rc = check_device();
+    if (rc != VA_OK) return rc;
+    va::NormArgs a = norm_args(p);
+    a.x = x; a.residual = residual; a.weight = weight; a.bias = bias; a.y = y; a.summed = summed; a.mean = mean; a.rstd = rstd;
+    a.codes = codes; a.scales = scales;
+    a.x_stride = p->x_stride;
+    if (codes) a.format = p->act8_format;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    ProfScope ps(VA_KERNEL_NORM, stream);
+    const hipError_t e = va::launch_norm_fwd(a, stream);
+    return e == hipSuccess ? VA_OK : hip_fail(e);
+}
+
+size_t varlen_attn_norm_bwd_workspace_bytes(const varlen_attn_norm_params* p) {
+    if (check_norm(p) != VA_OK) return 0;
+    const size_t wgs = va::norm_bwd_wgs((int64_t)p->total_tokens * p->rows_per_token, p->channels);
+    return (wgs * 2 * p->channels * sizeof(float) + 255) / 256 * 256;
+}
+
+int varlen_attn_norm_bwd(const varlen_attn_norm_params* p, const void* dy, const void* x, const void* codes, const float* scales,
+                         const float* mean, const float* rstd, const void* weight, const void* dsummed, void* dx, float* dweight,
+                         float* dbias, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    int rc = check_norm(p);
+    if (rc != VA_OK) return rc;
+    const int64_t width = (int64_t)p->rows_per_token * p->channels;
+    if (p->dy_stride < width || p->dx_stride < width || (x && p->x_stride < width)) return VA_ERR_BAD_SHAPE;
+    if (weight && any_null({dweight, dbias})) return VA_ERR_NULL_PTR;
+    const size_t wa = p->weight_type == VA_BF16 ? 2 : 4;
+    if (!aligned_to(wa, {weight}) || !aligned_to(4, {dweight, dbias})) return VA_ERR_MISALIGNED;
+    if (p->total_tokens == 0 && !weight) return VA_OK;
+    if (p->total_tokens > 0) {
+        if (any_null({dy, mean, rstd, dx}) || !x == !codes || !codes != !scales || (weight && !workspace)) return VA_ERR_NULL_PTR;
+        if (!aligned_to(2, {dy, x, dsummed, dx}) || !aligned_to(4, {mean, rstd, scales, workspace})) return VA_ERR_MISALIGNED;
+        if (weight && workspace_bytes < varlen_attn_norm_bwd_workspace_bytes(p)) return VA_ERR_WORKSPACE_TOO_SMALL;
+    }
+    rc = check_device();
+    if (rc != VA_OK) return rc;
+    va::NormArgs a = norm_args(p);
+    a.dy = dy; a.x = x; a.codes = const_cast<void*>(codes); a.scales = const_cast<float*>(scales);
+    a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+    a.weight = weight; a.dsummed = dsummed; a.dx = dx; a.dweight = dweight; a.dbias = dbias;
+    a.partial = (float*)workspace;
+    a.x_stride = p->x_stride; a.dy_stride = p->dy_stride; a.dx_stride = p->dx_stride;
+    if (codes) a.format = p->act8_format;
+    hipStream_t stream = (hipStream_t)hip_stream;
+    ProfScope ps(VA_KERNEL_NORM, stream);
+    const hipError_t e = va::launch_norm_bwd(a, stream);
+    return e == hipSuccess ? VA_OK : hip_fail(e);
 }
 
 const char* varlen_attn_status_string(int status) {

@@ -141,4 +141,57 @@ hipError_t launch_merge(const void* o_parts, bool parts_fp32, const float* lse_p
 hipError_t launch_bwd_dkdv(const BwdArgs& a, hipStream_t stream);
 hipError_t launch_bwd_dq(const BwdArgs& a, hipStream_t stream);
 
+// Rotary positions (va_rotary.hip).  Strides in elements between tokens; the channels of a token's heads lie side by side.
+struct RotaryArgs {
+    const uint16_t *q, *k, *v;  // bf16; v may be null
+    uint16_t *q_out, *k_out, *v_out;
+    int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride, v_out_stride;
+    const int32_t* positions;  // [num_axes, total_tokens]
+    const float* inv_freq;     // [num_pairs]
+    const int32_t* pair_axis;  // [num_pairs]
+    int total_tokens, num_q_heads, num_kv_heads, head_dim, num_pairs, num_axes;
+    bool interleaved, inverse;
+    int tokens_per_wg;  // (filled by the launch)
+};
+hipError_t launch_rotary(RotaryArgs a, hipStream_t stream);
+hipError_t launch_rotary_positions(int total_tokens, int num_segments, int merge, const int32_t* cu, const int32_t* grids,
+                                   const int32_t* first, int32_t* positions, hipStream_t stream);
+
+// Layer norm (va_norm.hip).  rows = tokens * rows_per_token; x, dy and dx have a stride in elements between tokens, everything
+// else lies row by row.
+struct NormArgs {
+    const void *x, *residual, *dy, *dsummed;
+    void *y, *summed, *dx;
+    const void *weight, *bias;
+    int weight_type;  // VA_BF16, VA_FP32
+    float *mean, *rstd;
+    void* codes;
+    float* scales;
+    int format;  // of codes; -1: none
+    float *partial, *dweight, *dbias;
+    int64_t rows, x_stride, dy_stride, dx_stride;
+    int rows_per_token, channels;
+    float eps;
+};
+int norm_bwd_wgs(int64_t rows, int channels);  // rows of partial sums the backward leaves, 2 * channels floats each
+hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream);
+hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream);
+
+// Activations in 8 bits (va_act8.hip).
+struct Act8Tensor {
+    void* values;  // bf16
+    void* codes;
+    float* scales;
+    int64_t rows, stride;  // stride: elements between tokens of `values`
+    int rows_per_token, channels;
+    uint32_t first_wg;  // (filled by the launch)
+};
+constexpr int ACT8_MAX_TENSORS = 8;
+struct Act8Args {
+    Act8Tensor t[ACT8_MAX_TENSORS];
+    int num, format;
+};
+hipError_t launch_act8_pack(const Act8Args& a, hipStream_t stream);
+hipError_t launch_act8_unpack(const Act8Args& a, hipStream_t stream);
+
 }  // namespace va
