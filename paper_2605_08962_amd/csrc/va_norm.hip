@@ -34,7 +34,7 @@ __device__ __forceinline__ void row_sum(float (&x)[N], float (*lds)[4][RowGroup<
 #pragma unroll
             for (int i = 0; i < N; ++i) lds[at][i][wave] = x[i];
         }
-        __syncthreads();
+        wg_barrier();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float s = lds[at][i][first];
@@ -46,15 +46,29 @@ __device__ __forceinline__ void row_sum(float (&x)[N], float (*lds)[4][RowGroup<
     }
 }
 
-// Eight weights from column `col` on, n of them there.
+// Eight values of weight or bias from column `col` on, n of them there, else `other`.
 template <bool WIDE>
-__device__ __forceinline__ void load_weights(const void* w, int type, int col, int n, float* x) {
+__device__ __forceinline__ void load_weights(const void* w, int type, int col, int n, float other, float* x) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = other;
+    if (!w) return;
     if (type == VA_BF16) {
         to_float8(load8<WIDE>((const uint16_t*)w + col, n), x);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = e < n ? ((const float*)w)[col + e] : 0.f;
     }
+}
+
+// Where row `row` of a tensor with a stride between tokens starts.
+__device__ __forceinline__ int64_t row_offset(const NormArgs& a, int64_t row, int64_t stride) {
+    if (stride == (int64_t)a.rows_per_token * a.channels) return row * a.channels;
+    if (a.rows_per_token == 1) return row * stride;
+    if (a.rows <= INT32_MAX) {  // (a division in 64 bits is 100 instructions, on rows of as few as 8 channels a lane)
+        const uint32_t r = (uint32_t)row, t = r / (uint32_t)a.rows_per_token;
+        return t * stride + (int64_t)(r - t * (uint32_t)a.rows_per_token) * a.channels;
+    }
+    return row / a.rows_per_token * stride + row % a.rows_per_token * a.channels;
 }
 
 template <int G, int NV, bool WIDE>
@@ -64,30 +78,52 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
     int at = 0;
     const int C = a.channels, lane = threadIdx.x % G;
     const int blocks = (C + kAct8Block - 1) / kAct8Block;
-    for (int64_t base = (int64_t)blockIdx.x * R::ROWS; base < a.rows; base += (int64_t)gridDim.x * R::ROWS) {
-        const int64_t row = base + threadIdx.x / G;
+    float w[NV][8], b[NV][8];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int col = 8 * (lane + j * G);
+        load_weights<WIDE>(a.weight, a.weight_type, col, C - col, 1.f, w[j]);
+        load_weights<WIDE>(a.bias, a.weight_type, col, C - col, 0.f, b[j]);
+    }
+    const int64_t step = (int64_t)gridDim.x * R::ROWS;
+    u32x4 xs[NV], rs[NV];
+    auto fetch = [&](int64_t row) {
+        const uint16_t* const x = (const uint16_t*)a.x + row_offset(a, row, a.x_stride);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int col = 8 * (lane + j * G), n = row < a.rows ? C - col : 0;
+            xs[j] = load8<WIDE>(x + col, n);
+            if (a.residual) rs[j] = load8<WIDE>((const uint16_t*)a.residual + row * C + col, n);
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / G;
+    fetch(row);
+    for (int64_t base = (int64_t)blockIdx.x * R::ROWS; base < a.rows; base += step, row += step) {
         const bool there = row < a.rows;
-        const int64_t token = row / a.rows_per_token;
-        const uint16_t* const x = (const uint16_t*)a.x + token * a.x_stride + (row % a.rows_per_token) * C;
         float h[NV][8];
+        u32x4 kept[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            kept[j] = xs[j];
+            to_float8(xs[j], h[j]);
+            if (a.residual) {
+                float r[8];
+                to_float8(rs[j], r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[j][e] += r[e];
+                kept[j] = to_bf16x8(h[j]);  // the stream goes on in bf16, and the norm is of what goes on
+                to_float8(kept[j], h[j]);
+            }
+        }
+        fetch(row + step);  // (in flight while this row is worked on)
         float sum[1] = {0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = 8 * (lane + j * G), n = there ? C - col : 0;
-            u32x4 w = load8<WIDE>(x + col, n);
-            to_float8(w, h[j]);
-            if (a.residual) {
-                float r[8];
-                to_float8(load8<WIDE>((const uint16_t*)a.residual + row * C + col, n), r);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[j][e] += r[e];
-                w = to_bf16x8(h[j]);  // the stream goes on in bf16, and the norm is of what goes on
-                store8<WIDE>((uint16_t*)a.summed + row * C + col, w, n);
-                to_float8(w, h[j]);
-            }
+            if (a.residual) store8<WIDE>((uint16_t*)a.summed + row * C + col, kept[j], n);
             if (a.format >= 0) {
                 constexpr int L = R::LANES < 16 ? R::LANES : 16;
-                const float s = act8_scale(lanes_max<L>(magnitude8(w)), a.format);
+                const float s = act8_scale(lanes_max<L>(magnitude8(kept[j])), a.format);
                 store_codes<WIDE>((uint8_t*)a.codes + row * C + col, act8_encode(h[j], s, a.format), n);
                 if (lane % L == 0 && n > 0) a.scales[row * blocks + col / kAct8Block] = s;
             }
@@ -103,7 +139,8 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 h[j][e] -= mean;
-                if (e < n) sq[0] += h[j][e] * h[j][e];
+                const float d = (WIDE ? n > 0 : e < n) ? h[j][e] : 0.f;
+                sq[0] += d * d;
             }
         }
         row_sum<G>(sq, lds, at);
@@ -115,15 +152,9 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = 8 * (lane + j * G), n = there ? C - col : 0;
-            float w[8], b[8], y[8];
-            if (a.weight) load_weights<WIDE>(a.weight, a.weight_type, col, n, w);
-            if (a.bias) load_weights<WIDE>(a.bias, a.weight_type, col, n, b);
+            float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                y[e] = h[j][e] * rstd;
-                if (a.weight) y[e] *= w[e];
-                if (a.bias) y[e] += b[e];
-            }
+            for (int e = 0; e < 8; ++e) y[e] = h[j][e] * rstd * w[j][e] + b[j][e];
             store8<WIDE>((uint16_t*)a.y + row * C + col, to_bf16x8(y), n);
         }
     }
@@ -138,39 +169,76 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
     int at = 0;
     const int C = a.channels, lane = threadIdx.x % G;
     const int blocks = (C + kAct8Block - 1) / kAct8Block;
+    float w[NV][8];
     float dw[NV][8] = {}, db[NV][8] = {};
-    for (int64_t base = (int64_t)blockIdx.x * R::ROWS; base < a.rows; base += (int64_t)gridDim.x * R::ROWS) {
-        const int64_t row = base + threadIdx.x / G;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int col = 8 * (lane + j * G);
+        load_weights<WIDE>(a.weight, a.weight_type, col, C - col, 1.f, w[j]);
+    }
+    const int64_t step = (int64_t)gridDim.x * R::ROWS;
+    struct Row {
+        u32x4 x[NV], dy[NV];
+        u32x2 codes[NV];
+        float scale[NV], mean, rstd;
+    } next;
+    auto fetch = [&](int64_t row) {
         const bool there = row < a.rows;
-        const int64_t token = row / a.rows_per_token, inner = (row % a.rows_per_token) * C;
-        const float mean = there ? a.mean[row] : 0.f, rstd = there ? a.rstd[row] : 0.f;
+        next.mean = there ? a.mean[row] : 0.f;
+        next.rstd = there ? a.rstd[row] : 0.f;
+        const uint16_t* const dy = (const uint16_t*)a.dy + row_offset(a, row, a.dy_stride);
+        const uint16_t* const x = FORMAT < 0 ? (const uint16_t*)a.x + row_offset(a, row, a.x_stride) : nullptr;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int col = 8 * (lane + j * G), n = there ? C - col : 0;
+            if constexpr (FORMAT < 0) {
+                next.x[j] = load8<WIDE>(x + col, n);
+            } else {
+                next.scale[j] = n > 0 ? a.scales[row * blocks + col / kAct8Block] : 0.f;
+                next.codes[j] = load_codes<WIDE>((const uint8_t*)a.codes + row * C + col, n);
+            }
+            next.dy[j] = load8<WIDE>(dy + col, n);
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / G;
+    fetch(row);
+    for (int64_t base = (int64_t)blockIdx.x * R::ROWS; base < a.rows; base += step, row += step) {
+        const bool there = row < a.rows;
+        const float mean = next.mean, rstd = next.rstd;
         float n[NV][8], g[NV][8];
+        u32x4 ds[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if constexpr (FORMAT < 0) to_float8(next.x[j], n[j]);
+            else act8_decode(next.codes[j], next.scale[j], FORMAT, n[j]);
+            to_float8(next.dy[j], g[j]);
+        }
+        fetch(row + step);  // (in flight while this row is worked on)
+        if (a.dsummed) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int col = 8 * (lane + j * G);
+                ds[j] = load8<WIDE>((const uint16_t*)a.dsummed + row * C + col, there ? C - col : 0);
+            }
+        }
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int col = 8 * (lane + j * G), left = there ? C - col : 0;
-            if (FORMAT < 0) {
-                to_float8(load8<WIDE>((const uint16_t*)a.x + token * a.x_stride + inner + col, left), n[j]);
-            } else {
-                const float s = left > 0 ? a.scales[row * blocks + col / kAct8Block] : 0.f;
-                act8_decode(load_codes<WIDE>((const uint8_t*)a.codes + row * C + col, left), s, FORMAT, n[j]);
-            }
-            float dy[8];
-            to_float8(load8<WIDE>((const uint16_t*)a.dy + token * a.dy_stride + inner + col, left), dy);
-            float w[8];
-            if (a.weight) load_weights<WIDE>(a.weight, a.weight_type, col, left, w);
+            const int left = C - 8 * (lane + j * G);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                n[j][e] = e < left ? (n[j][e] - mean) * rstd : 0.f;
-                g[j][e] = a.weight ? dy[e] * w[e] : dy[e];
-                dw[j][e] += dy[e] * n[j][e];
-                db[j][e] += dy[e];
+                const float dy = g[j][e];
+                n[j][e] = (WIDE ? left > 0 : e < left) ? (n[j][e] - mean) * rstd : 0.f;
+                g[j][e] = dy * w[j][e];
+                dw[j][e] += dy * n[j][e];
+                db[j][e] += dy;
                 sum[0] += g[j][e];
                 sum[1] += g[j][e] * n[j][e];
             }
         }
         row_sum<G>(sum, lds, at);
         const float c0 = sum[0] / (float)C, c1 = sum[1] / (float)C;
+        uint16_t* const out = (uint16_t*)a.dx + row_offset(a, row, a.dx_stride);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = 8 * (lane + j * G), left = there ? C - col : 0;
@@ -179,11 +247,11 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
             for (int e = 0; e < 8; ++e) dx[e] = rstd * (g[j][e] - c0 - n[j][e] * c1);
             if (a.dsummed) {
                 float r[8];
-                to_float8(load8<WIDE>((const uint16_t*)a.dsummed + row * C + col, left), r);
+                to_float8(ds[j], r);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dx[e] += r[e];
             }
-            store8<WIDE>((uint16_t*)a.dx + token * a.dx_stride + inner + col, to_bf16x8(dx), left);
+            store8<WIDE>(out + col, to_bf16x8(dx), left);
         }
     }
     if (!a.weight) return;
@@ -197,42 +265,45 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
                 const int c = 8 * (lane + j * G) + e;
                 if (c < C) { out[c] = dw[j][e]; out[C + c] = db[j][e]; }
             }
-        return;
-    }
-    for (int s = 0; s < R::ROWS; ++s) {
-        if ((int)threadIdx.x / G == s) {
+    } else {
+        for (int s = 0; s < R::ROWS; ++s) {
+            if ((int)threadIdx.x / G == s) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+                for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int at8 = ((j * 8 + e) * G + lane) % (R::ROWS > 1 ? 8 * NV * G : 1);
-                    part[0][at8] = s ? part[0][at8] + dw[j][e] : dw[j][e];
-                    part[1][at8] = s ? part[1][at8] + db[j][e] : db[j][e];
-                }
+                    for (int e = 0; e < 8; ++e) {
+                        const int i = (j * 8 + e) * G + lane;
+                        part[0][i] = s ? part[0][i] + dw[j][e] : dw[j][e];
+                        part[1][i] = s ? part[1][i] + db[j][e] : db[j][e];
+                    }
+            }
+            __syncthreads();
         }
-        __syncthreads();
-    }
-    for (int c = threadIdx.x; c < C; c += R::THREADS) {
-        const int at8 = ((c / 8 / G) * 8 + c % 8) * G + c / 8 % G;
-        out[c] = part[0][at8];
-        out[C + c] = part[1][at8];
+        for (int c = threadIdx.x; c < C; c += R::THREADS) {
+            const int i = ((c / 8 / G) * 8 + c % 8) * G + c / 8 % G;
+            out[c] = part[0][i];
+            out[C + c] = part[1][i];
+        }
     }
 }
 
-// dw and db from the workgroups' partial sums [wgs, 2, C]: 32 columns a workgroup, 8 threads a column.
-__global__ void __launch_bounds__(256) norm_sum_kernel(const float* __restrict__ partial, int wgs, int C, float* __restrict__ dweight,
-                                                       float* __restrict__ dbias) {
-    __shared__ float lds[8][32];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, part = threadIdx.x / 32, which = blockIdx.y;
+// dw and db from the workgroups' partial sums [wgs, 2 C]: 32 columns a workgroup, 32 threads a column.
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const float* __restrict__ partial, int wgs, int C, float* __restrict__ dweight,
+                                                        float* __restrict__ dbias) {
+    __shared__ float lds[32][33];
+    const int x = threadIdx.x % 32, y = threadIdx.x / 32, c = blockIdx.x * 32 + x;
     float s = 0.f;
-    if (c < C)
-        for (int i = part; i < wgs; i += 8) s += partial[((size_t)i * 2 + which) * C + c];
-    lds[part][threadIdx.x % 32] = s;
+    if (c < 2 * C) {
+#pragma unroll 8
+        for (int i = y; i < wgs; i += 32) s += partial[(size_t)i * 2 * C + c];
+    }
+    lds[y][x] = s;
     __syncthreads();
-    if (part == 0 && c < C) {
+    if (y == 0 && c < 2 * C) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) s += lds[i][threadIdx.x];
-        (which ? dbias : dweight)[c] = s;
+        for (int i = 1; i < 32; ++i) s += lds[i][x];
+        if (c < C) dweight[c] = s;
+        else dbias[c - C] = s;
     }
 }
 
@@ -255,10 +326,10 @@ static int norm_rows_per_wg(int C) {
 #undef VA_NORM_GO
 }
 
-// Workgroups of the backward pass: what fits the chip at once, as long as there are rows.
+// Workgroups of the backward pass: up to what fits the chip at once, with four rows a thread group as soon as every CU has one.
 int norm_bwd_wgs(int64_t rows, int C) {
-    const int64_t r = norm_rows_per_wg(C);
-    const int64_t wgs = (rows + r - 1) / r;
+    const int64_t r = norm_rows_per_wg(C), one = (rows + r - 1) / r, four = (rows + 4 * r - 1) / (4 * r);
+    const int64_t wgs = four > 256 ? four : one < 256 ? one : 256;
     return (int)(wgs < 1024 ? wgs : 1024);
 }
 
@@ -298,7 +369,7 @@ hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
         if (e != hipSuccess) return e;
     }
     if (a.weight)
-        hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((C + 31) / 32), 2), dim3(256), 0, stream, a.partial, wgs, C, a.dweight,
+        hipLaunchKernelGGL(norm_sum_kernel, dim3((unsigned)((2 * C + 31) / 32)), dim3(1024), 0, stream, a.partial, wgs, C, a.dweight,
                            a.dbias);
     return hipGetLastError();
 }

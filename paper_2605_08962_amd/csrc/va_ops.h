@@ -104,11 +104,18 @@ __device__ __forceinline__ float act8_scale(uint32_t magnitude, int format) {
     return magnitude >= 0x7f80u ? __uint_as_float(0x7fc00000u) : s;
 }
 __device__ __forceinline__ u32x2 act8_encode(const float* x, float scale, int format) {
+#pragma clang fp contract(off)  // (the product with inv is rounded by itself: that is the format's definition)
     const float inv = 1.f / scale;
     u32x2 w = {0, 0};
     if (format == VA_ACT8_INT8) {
+        // adding 1.5 * 2^23 rounds to an integer, to nearest even, and leaves it in the lowest bits
+        uint32_t u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)(int)rintf(x[e] * inv) & 255u) << (8 * (e & 3));
+        for (int e = 0; e < 8; ++e) u[e] = __float_as_uint(x[e] * inv + 0x1.8p23f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            w[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[4 * i + 3], u[4 * i + 2], 0x0c0c0400),
+                                         __builtin_amdgcn_perm(u[4 * i + 1], u[4 * i], 0x0c0c0400), 0x05040100);
     } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -120,8 +127,10 @@ __device__ __forceinline__ u32x2 act8_encode(const float* x, float scale, int fo
 }
 __device__ __forceinline__ void act8_decode(const u32x2& w, float scale, int format, float* x) {
     if (format == VA_ACT8_INT8) {
+        // code + 128 as an unsigned byte: one conversion, and 128 scale comes off again exactly, with the one rounding of the product
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (float)((int)(w[e >> 2] << (24 - 8 * (e & 3))) >> 24) * scale;
+        for (int e = 0; e < 8; ++e)
+            x[e] = fmaf((float)(((w[e >> 2] ^ 0x80808080u) >> (8 * (e & 3))) & 255u), scale, -128.f * scale);
     } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
