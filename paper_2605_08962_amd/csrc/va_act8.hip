@@ -6,8 +6,8 @@
 namespace va {
 
 // G lanes (8 where every row is at most 64 channels, else 16) take one block of a row, 8 channels each; one thread handles one
-// such run.  WIDE: see load8.
-template <int G, bool WIDE, bool PACK>
+// such run.  MODE: see load8.
+template <int G, int MODE, bool PACK>
 __global__ void __launch_bounds__(256) act8_kernel(Act8Args a) {
     int ti = 0;
     while (ti + 1 < a.num && blockIdx.x >= a.t[ti + 1].first_wg) ++ti;
@@ -24,16 +24,16 @@ __global__ void __launch_bounds__(256) act8_kernel(Act8Args a) {
     uint8_t* const codes = (uint8_t*)x.codes + row * x.channels + col;
     float* const scale = x.scales + row * blocks + block;
     if (PACK) {
-        const u32x4 w = load8<WIDE>(v, n);
+        const u32x4 w = load8<MODE>(v, n);
         float f[8];
         to_float8(w, f);
         const float s = act8_scale(lanes_max<G>(magnitude8(w)), a.format);
-        store_codes<WIDE>(codes, act8_encode(f, s, a.format), n);
+        store_codes<MODE>(codes, act8_encode(f, s, a.format), n);
         if (lane == 0 && n > 0) *scale = s;
     } else if (n > 0) {
         float f[8];
-        act8_decode(load_codes<WIDE>(codes, n), *scale, a.format, f);
-        store8<WIDE>(v, to_bf16x8(f), n);
+        act8_decode(load_codes<MODE>(codes, n), *scale, a.format, f);
+        store8<MODE>(v, to_bf16x8(f), n);
     }
 }
 
@@ -43,7 +43,7 @@ static hipError_t launch_act8(Act8Args a, hipStream_t stream) {
     int most = 0;
     for (int i = 0; i < a.num; ++i) {
         const Act8Tensor& x = a.t[i];
-        wide = wide && (uintptr_t)x.values % 16 == 0 && (uintptr_t)x.codes % 8 == 0 && x.stride % 8 == 0 && x.channels % 8 == 0;
+        wide = wide && x.channels % 8 == 0;
         most = x.channels > most ? x.channels : most;
     }
     const int G = most <= 64 ? 8 : 16;
@@ -56,10 +56,10 @@ static hipError_t launch_act8(Act8Args a, hipStream_t stream) {
     if (wgs == 0) return hipSuccess;
     if (wgs > INT32_MAX) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)wgs), block(256);
-    if (G == 8 && wide) hipLaunchKernelGGL((act8_kernel<8, true, PACK>), grid, block, 0, stream, a);
-    else if (G == 8) hipLaunchKernelGGL((act8_kernel<8, false, PACK>), grid, block, 0, stream, a);
-    else if (wide) hipLaunchKernelGGL((act8_kernel<16, true, PACK>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((act8_kernel<16, false, PACK>), grid, block, 0, stream, a);
+    if (G == 8 && wide) hipLaunchKernelGGL((act8_kernel<8, WIDE, PACK>), grid, block, 0, stream, a);
+    else if (G == 8) hipLaunchKernelGGL((act8_kernel<8, RAGGED, PACK>), grid, block, 0, stream, a);
+    else if (wide) hipLaunchKernelGGL((act8_kernel<16, WIDE, PACK>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((act8_kernel<16, RAGGED, PACK>), grid, block, 0, stream, a);
     return hipGetLastError();
 }
 

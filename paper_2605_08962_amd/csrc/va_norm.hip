@@ -46,19 +46,34 @@ __device__ __forceinline__ void row_sum(float (&x)[N], float (*lds)[4][RowGroup<
     }
 }
 
-// Eight values of weight or bias from column `col` on, n of them there, else `other`.
-template <bool WIDE>
-__device__ __forceinline__ void load_weights(const void* w, int type, int col, int n, float other, float* x) {
+// Weight or bias in fp32 in LDS, as threads of a row read them: 16 bytes a thread, neighbours side by side.  (In registers they
+// cost 8 a run and with that a wave per SIMD or two, which is bytes in flight.)
+template <int G, int NV>
+struct Weights {
+    float4 x[NV * 2 * G];
+    // `w`, or `other` everywhere without one, and zeros behind the row's end; a barrier has to follow.
+    template <int MODE>
+    __device__ __forceinline__ void fill(const void* w, int type, int C, float other) {
+        for (int i = threadIdx.x; i < NV * G; i += RowGroup<G>::THREADS) {
+            const int n = C - 8 * i;
+            float v[8];
+            if (type == VA_BF16 && w) {
+                to_float8(load8<MODE>((const uint16_t*)w + 8 * i, n), v);
+            } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = other;
-    if (!w) return;
-    if (type == VA_BF16) {
-        to_float8(load8<WIDE>((const uint16_t*)w + col, n), x);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = e < n ? ((const float*)w)[col + e] : 0.f;
+                for (int e = 0; e < 8; ++e) v[e] = e >= n ? 0.f : w ? ((const float*)w)[8 * i + e] : other;
+            }
+            const int at = i / G * 2 * G + i % G;
+            x[at] = float4{v[0], v[1], v[2], v[3]};
+            x[at + G] = float4{v[4], v[5], v[6], v[7]};
+        }
     }
-}
+    __device__ __forceinline__ void get(int j, int lane, float* v) const {
+        const float4 a = x[2 * j * G + lane], b = x[(2 * j + 1) * G + lane];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+};
 
 // Where row `row` of a tensor with a stride between tokens starts.
 __device__ __forceinline__ int64_t row_offset(const NormArgs& a, int64_t row, int64_t stride) {
@@ -71,20 +86,14 @@ __device__ __forceinline__ int64_t row_offset(const NormArgs& a, int64_t row, in
     return row / a.rows_per_token * stride + row % a.rows_per_token * a.channels;
 }
 
-template <int G, int NV, bool WIDE>
+template <int G, int NV, int MODE>
 __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs a) {
     using R = RowGroup<G>;
     __shared__ float lds[2][4][R::THREADS / 64];
+    __shared__ Weights<G, NV> weight, bias;
     int at = 0;
     const int C = a.channels, lane = threadIdx.x % G;
     const int blocks = (C + kAct8Block - 1) / kAct8Block;
-    float w[NV][8], b[NV][8];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int col = 8 * (lane + j * G);
-        load_weights<WIDE>(a.weight, a.weight_type, col, C - col, 1.f, w[j]);
-        load_weights<WIDE>(a.bias, a.weight_type, col, C - col, 0.f, b[j]);
-    }
     const int64_t step = (int64_t)gridDim.x * R::ROWS;
     u32x4 xs[NV], rs[NV];
     auto fetch = [&](int64_t row) {
@@ -92,56 +101,57 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = 8 * (lane + j * G), n = row < a.rows ? C - col : 0;
-            xs[j] = load8<WIDE>(x + col, n);
-            if (a.residual) rs[j] = load8<WIDE>((const uint16_t*)a.residual + row * C + col, n);
+            xs[j] = load8<MODE>(x + col, n);
+            if (a.residual) rs[j] = load8<MODE>((const uint16_t*)a.residual + row * C + col, n);
         }
     };
     int64_t row = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / G;
     fetch(row);
+    weight.template fill<MODE>(a.weight, a.weight_type, C, 1.f);
+    bias.template fill<MODE>(a.bias, a.weight_type, C, 0.f);
+    __syncthreads();
     for (int64_t base = (int64_t)blockIdx.x * R::ROWS; base < a.rows; base += step, row += step) {
         const bool there = row < a.rows;
         float h[NV][8];
-        u32x4 kept[NV];
+        float sum[1] = {0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            kept[j] = xs[j];
-            to_float8(xs[j], h[j]);
+            const int col = 8 * (lane + j * G), n = there ? C - col : 0;
+            u32x4 kept = xs[j];
+            to_float8(kept, h[j]);
             if (a.residual) {
                 float r[8];
                 to_float8(rs[j], r);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) h[j][e] += r[e];
-                kept[j] = to_bf16x8(h[j]);  // the stream goes on in bf16, and the norm is of what goes on
-                to_float8(kept[j], h[j]);
+                kept = to_bf16x8(h[j]);  // the stream goes on in bf16, and the norm is of what goes on
+                to_float8(kept, h[j]);
+                store8<MODE>((uint16_t*)a.summed + row * C + col, kept, n);
             }
-        }
-        fetch(row + step);  // (in flight while this row is worked on)
-        float sum[1] = {0.f};
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int col = 8 * (lane + j * G), n = there ? C - col : 0;
-            if (a.residual) store8<WIDE>((uint16_t*)a.summed + row * C + col, kept[j], n);
             if (a.format >= 0) {
                 constexpr int L = R::LANES < 16 ? R::LANES : 16;
-                const float s = act8_scale(lanes_max<L>(magnitude8(kept[j])), a.format);
-                store_codes<WIDE>((uint8_t*)a.codes + row * C + col, act8_encode(h[j], s, a.format), n);
+                const float s = act8_scale(lanes_max<L>(magnitude8(kept)), a.format);
+                store_codes<MODE>((uint8_t*)a.codes + row * C + col, act8_encode(h[j], s, a.format), n);
                 if (lane % L == 0 && n > 0) a.scales[row * blocks + col / kAct8Block] = s;
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[0] += h[j][e];
         }
+        fetch(row + step);  // (in flight while this row is worked on)
         row_sum<G>(sum, lds, at);
         const float mean = sum[0] / (float)C;
         float sq[1] = {0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int n = C - 8 * (lane + j * G);
+            float run = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 h[j][e] -= mean;
-                const float d = (WIDE ? n > 0 : e < n) ? h[j][e] : 0.f;
-                sq[0] += d * d;
+                const float d = MODE != RAGGED || e < n ? h[j][e] : 0.f;
+                run += d * d;
             }
+            sq[0] += n > 0 ? run : 0.f;
         }
         row_sum<G>(sq, lds, at);
         const float rstd = 1.f / sqrtf(sq[0] / (float)C + a.eps);
@@ -152,30 +162,29 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = 8 * (lane + j * G), n = there ? C - col : 0;
-            float y[8];
+            float y[8], w[8], b[8];
+            weight.get(j, lane, w);
+            bias.get(j, lane, b);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = h[j][e] * rstd * w[j][e] + b[j][e];
-            store8<WIDE>((uint16_t*)a.y + row * C + col, to_bf16x8(y), n);
+            for (int e = 0; e < 8; ++e) y[e] = h[j][e] * rstd * w[e] + b[e];
+            store8<MODE>((uint16_t*)a.y + row * C + col, to_bf16x8(y), n);
         }
     }
 }
 
 // FORMAT: -1 the row in bf16, else its 8-bit codes.
-template <int G, int NV, bool WIDE, int FORMAT>
+template <int G, int NV, int MODE, int FORMAT>
 __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs a) {
     using R = RowGroup<G>;
     __shared__ float lds[2][4][R::THREADS / 64];
-    __shared__ float part[2][R::ROWS > 1 ? 8 * NV * G : 1];
+    __shared__ union {
+        Weights<G, NV> weight;
+        float part[2][R::ROWS > 1 ? 8 * NV * G : 1];  // (behind the last row)
+    } u;
     int at = 0;
     const int C = a.channels, lane = threadIdx.x % G;
     const int blocks = (C + kAct8Block - 1) / kAct8Block;
-    float w[NV][8];
     float dw[NV][8] = {}, db[NV][8] = {};
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int col = 8 * (lane + j * G);
-        load_weights<WIDE>(a.weight, a.weight_type, col, C - col, 1.f, w[j]);
-    }
     const int64_t step = (int64_t)gridDim.x * R::ROWS;
     struct Row {
         u32x4 x[NV], dy[NV];
@@ -192,66 +201,82 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
         for (int j = 0; j < NV; ++j) {
             const int col = 8 * (lane + j * G), n = there ? C - col : 0;
             if constexpr (FORMAT < 0) {
-                next.x[j] = load8<WIDE>(x + col, n);
+                next.x[j] = load8<MODE>(x + col, n);
             } else {
                 next.scale[j] = n > 0 ? a.scales[row * blocks + col / kAct8Block] : 0.f;
-                next.codes[j] = load_codes<WIDE>((const uint8_t*)a.codes + row * C + col, n);
+                next.codes[j] = load_codes<MODE>((const uint8_t*)a.codes + row * C + col, n);
             }
-            next.dy[j] = load8<WIDE>(dy + col, n);
+            next.dy[j] = load8<MODE>(dy + col, n);
         }
     };
     int64_t row = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / G;
     fetch(row);
+    u.weight.template fill<MODE>(a.weight, a.weight_type, C, 1.f);
+    __syncthreads();
     for (int64_t base = (int64_t)blockIdx.x * R::ROWS; base < a.rows; base += step, row += step) {
         const bool there = row < a.rows;
-        const float mean = next.mean, rstd = next.rstd;
-        float n[NV][8], g[NV][8];
-        u32x4 ds[NV];
+        Row now = next;
+        // d = h - mean, dy and g = dy w of run j.  Formed twice, for the sums and for dx: kept, they would be 24 registers a run
+        // instead of 8 or 6, which is a wave per SIMD or two.  Behind the row's end dy, and so g, is zero.
+        auto run = [&](int j, float* d, float* dy, float* g) {
+            if constexpr (FORMAT < 0) {
+                to_float8(now.x[j], d);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if constexpr (FORMAT < 0) to_float8(next.x[j], n[j]);
-            else act8_decode(next.codes[j], next.scale[j], FORMAT, n[j]);
-            to_float8(next.dy[j], g[j]);
-        }
+                for (int e = 0; e < 8; ++e) d[e] -= now.mean;
+            } else {
+                act8_decode(now.codes[j], now.scale[j], FORMAT, d, now.mean);
+            }
+            to_float8(now.dy[j], dy);
+            u.weight.get(j, lane, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] *= dy[e];
+        };
+        u32x4 ds[NV];
         fetch(row + step);  // (in flight while this row is worked on)
         if (a.dsummed) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int col = 8 * (lane + j * G);
-                ds[j] = load8<WIDE>((const uint16_t*)a.dsummed + row * C + col, there ? C - col : 0);
+                ds[j] = load8<MODE>((const uint16_t*)a.dsummed + row * C + col, there ? C - col : 0);
             }
         }
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int left = C - 8 * (lane + j * G);
+            float d[8], dy[8], g[8];
+            run(j, d, dy, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float dy = g[j][e];
-                n[j][e] = (WIDE ? left > 0 : e < left) ? (n[j][e] - mean) * rstd : 0.f;
-                g[j][e] = dy * w[j][e];
-                dw[j][e] += dy * n[j][e];
-                db[j][e] += dy;
-                sum[0] += g[j][e];
-                sum[1] += g[j][e] * n[j][e];
+                dw[j][e] += dy[e] * now.rstd * d[e];
+                db[j][e] += dy[e];
+                sum[0] += g[e];
+                sum[1] += g[e] * d[e];
             }
         }
         row_sum<G>(sum, lds, at);
-        const float c0 = sum[0] / (float)C, c1 = sum[1] / (float)C;
+        // dx = rstd (g - sum g / C - n sum(g n) / C) with n = d rstd
+        const float c0 = -now.rstd * (sum[0] / (float)C), c1 = -now.rstd * (now.rstd * (now.rstd * sum[1] / (float)C));
         uint16_t* const out = (uint16_t*)a.dx + row_offset(a, row, a.dx_stride);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {  // (the compiler must not see that it has formed them before)
+            if constexpr (FORMAT < 0) asm volatile("" : "+v"(now.x[j]));
+            else asm volatile("" : "+v"(now.codes[j]));
+            asm volatile("" : "+v"(now.dy[j]) : : "memory");
+        }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = 8 * (lane + j * G), left = there ? C - col : 0;
-            float dx[8];
+            float dx[8], d[8], dy[8], g[8];
+            run(j, d, dy, g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dx[e] = rstd * (g[j][e] - c0 - n[j][e] * c1);
+            for (int e = 0; e < 8; ++e) dx[e] = g[e] * now.rstd + (d[e] * c1 + c0);
             if (a.dsummed) {
                 float r[8];
                 to_float8(ds[j], r);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dx[e] += r[e];
             }
-            store8<WIDE>(out + col, to_bf16x8(dx), left);
+            store8<MODE>(out + col, to_bf16x8(dx), left);
         }
     }
     if (!a.weight) return;
@@ -266,6 +291,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
                 if (c < C) { out[c] = dw[j][e]; out[C + c] = db[j][e]; }
             }
     } else {
+        __syncthreads();  // (the weights are in the way)
         for (int s = 0; s < R::ROWS; ++s) {
             if ((int)threadIdx.x / G == s) {
 #pragma unroll
@@ -273,16 +299,16 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int i = (j * 8 + e) * G + lane;
-                        part[0][i] = s ? part[0][i] + dw[j][e] : dw[j][e];
-                        part[1][i] = s ? part[1][i] + db[j][e] : db[j][e];
+                        u.part[0][i] = s ? u.part[0][i] + dw[j][e] : dw[j][e];
+                        u.part[1][i] = s ? u.part[1][i] + db[j][e] : db[j][e];
                     }
             }
             __syncthreads();
         }
         for (int c = threadIdx.x; c < C; c += R::THREADS) {
             const int i = ((c / 8 / G) * 8 + c % 8) * G + c / 8 % G;
-            out[c] = part[0][i];
-            out[C + c] = part[1][i];
+            out[c] = u.part[0][i];
+            out[C + c] = u.part[1][i];
         }
     }
 }
@@ -307,60 +333,69 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* __restrict_
     }
 }
 
-static bool norm_wide(const NormArgs& a) {
-    const uint64_t bits = (uint64_t)(uintptr_t)a.x | (uintptr_t)a.residual | (uintptr_t)a.y | (uintptr_t)a.summed | (uintptr_t)a.dy |
-                          (uintptr_t)a.dsummed | (uintptr_t)a.dx | (uintptr_t)a.weight | (uintptr_t)a.bias | 2 * (uintptr_t)a.codes |
-                          2 * (uint64_t)(a.x_stride | a.dy_stride | a.dx_stride | a.channels);
-    return bits % 16 == 0;
+// Threads a row, runs a thread, workgroups a CU forward and backward.  Rows of up to 2048 channels stay in one wave, whose sums need
+// no barrier.  Two workgroups a CU that read ahead are more than the memory needs where rows are long, and more of them are slower:
+// forward / backward TB/s with 1, 2, 3, 4, 8 a CU, streaming,
+//   178572 x 1024   3.90 5.83 5.61 5.42 5.27 / 3.79 5.81 5.58 5.03 5.45        65537 x 1280   4.04 5.61 5.34 5.37 5.44 / 3.60 5.42 4.35 5.02 4.54
+//   32768 x 32 heads of 128   2.32 3.88 5.10 5.49 4.71 / 2.54 4.35 5.31 5.37 5.33        16000 x 8000   4.50 5.56 4.76 5.30 4.90 / 5.22 4.75 4.31 3.95 2.97
+#define VA_NORM_SHAPES(GO) \
+    if (C <= 64) GO(8, 1, 4, 4) else if (C <= 128) GO(16, 1, 4, 4) else if (C <= 256) GO(32, 1, 4, 4) else if (C <= 512) GO(64, 1, 4, 4) \
+    else if (C <= 1024) GO(64, 2, 2, 2) else if (C <= 1536) GO(64, 3, 2, 2) else if (C <= 2048) GO(64, 4, 2, 2) \
+    else if (C <= 4096) GO(256, 2, 2, 2) else if (C <= 8192) GO(256, 4, 2, 1) else GO(1024, 2, 1, 1)
+constexpr int CUS = 256;
+
+// Workgroups: as many as that, with two rows a thread group as soon as every CU has one.
+static int64_t norm_wgs(int64_t rows, int rows_per_wg, int wgs_per_cu) {
+    const int64_t one = (rows + rows_per_wg - 1) / rows_per_wg, two = (rows + 2 * rows_per_wg - 1) / (2 * rows_per_wg);
+    const int64_t wgs = two > CUS ? two : one < CUS ? one : CUS;
+    return wgs < wgs_per_cu * CUS ? wgs : wgs_per_cu * CUS;
 }
 
-// Threads a row and runs a thread: rows of up to 2048 channels stay in one wave, whose sums need no barrier.
-#define VA_NORM_SHAPES(GO) \
-    if (C <= 64) GO(8, 1) else if (C <= 128) GO(16, 1) else if (C <= 256) GO(32, 1) else if (C <= 512) GO(64, 1) \
-    else if (C <= 1024) GO(64, 2) else if (C <= 1536) GO(64, 3) else if (C <= 2048) GO(64, 4) else if (C <= 4096) GO(256, 2) \
-    else if (C <= 8192) GO(256, 4) else GO(1024, 2)
-
-static int norm_rows_per_wg(int C) {
-#define VA_NORM_GO(G, NV) return RowGroup<G>::ROWS;
+int norm_bwd_wgs(int64_t rows, int C) {
+#define VA_NORM_GO(G, NV, FWD, BWD) return (int)norm_wgs(rows, RowGroup<G>::ROWS, BWD);
     VA_NORM_SHAPES(VA_NORM_GO)
 #undef VA_NORM_GO
 }
 
-// Workgroups of the backward pass: up to what fits the chip at once, with four rows a thread group as soon as every CU has one.
-int norm_bwd_wgs(int64_t rows, int C) {
-    const int64_t r = norm_rows_per_wg(C), one = (rows + r - 1) / r, four = (rows + 4 * r - 1) / (4 * r);
-    const int64_t wgs = four > 256 ? four : one < 256 ? one : 256;
-    return (int)(wgs < 1024 ? wgs : 1024);
+// What is moved past the caches: more than the last one's 256 MB, which nobody finds there again.
+static int norm_mode(const NormArgs& a, int bytes_per_channel) {
+    if (a.channels % 8) return RAGGED;
+    return a.channels % 64 == 0 && a.rows * a.channels * bytes_per_channel > (int64_t)256 << 20 ? STREAM : WIDE;
 }
 
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) {
-    const int C = a.channels;
-    const bool wide = norm_wide(a);
-    const int64_t r = norm_rows_per_wg(C), want = (a.rows + r - 1) / r;
-    const dim3 grid((unsigned)(want < 2048 ? want : 2048));
-#define VA_NORM_GO(G, NV)                                                                                                     \
-    {                                                                                                                         \
-        if (wide) hipLaunchKernelGGL((norm_fwd_kernel<G, NV, true>), grid, dim3(RowGroup<G>::THREADS), 0, stream, a);          \
-        else hipLaunchKernelGGL((norm_fwd_kernel<G, NV, false>), grid, dim3(RowGroup<G>::THREADS), 0, stream, a);              \
+    const int C = a.channels, mode = norm_mode(a, a.residual ? 8 : 4);
+#define VA_NORM_FWD(G, NV, MODE) hipLaunchKernelGGL((norm_fwd_kernel<G, NV, MODE>), grid, dim3(RowGroup<G>::THREADS), 0, stream, a)
+#define VA_NORM_GO(G, NV, FWD, BWD)                                             \
+    {                                                                           \
+        const dim3 grid((unsigned)norm_wgs(a.rows, RowGroup<G>::ROWS, FWD));    \
+        if (mode == STREAM) VA_NORM_FWD(G, NV, STREAM);                         \
+        else if (mode == WIDE) VA_NORM_FWD(G, NV, WIDE);                        \
+        else VA_NORM_FWD(G, NV, RAGGED);                                        \
     }
     VA_NORM_SHAPES(VA_NORM_GO)
 #undef VA_NORM_GO
+#undef VA_NORM_FWD
     return hipGetLastError();
 }
 
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t stream) {
-    const int C = a.channels;
-    const bool wide = norm_wide(a);
+    const int C = a.channels, mode = norm_mode(a, a.dsummed ? 8 : a.format < 0 ? 6 : 5);
     const int wgs = norm_bwd_wgs(a.rows, C);
     if (wgs) {
         const dim3 grid((unsigned)wgs);
-#define VA_NORM_BWD(G, NV, WIDE, FORMAT) \
-    hipLaunchKernelGGL((norm_bwd_kernel<G, NV, WIDE, FORMAT>), grid, dim3(RowGroup<G>::THREADS), 0, stream, a)
-#define VA_NORM_FORMAT(G, NV, WIDE)                                                  \
-    if (a.format < 0) VA_NORM_BWD(G, NV, WIDE, -1);                                  \
-    else if (a.format == VA_ACT8_INT8) VA_NORM_BWD(G, NV, WIDE, VA_ACT8_INT8);       \
-    else VA_NORM_BWD(G, NV, WIDE, VA_ACT8_E4M3);
-#define VA_NORM_GO(G, NV) { if (wide) { VA_NORM_FORMAT(G, NV, true) } else { VA_NORM_FORMAT(G, NV, false) } }
+#define VA_NORM_BWD(G, NV, MODE, FORMAT) \
+    hipLaunchKernelGGL((norm_bwd_kernel<G, NV, MODE, FORMAT>), grid, dim3(RowGroup<G>::THREADS), 0, stream, a)
+#define VA_NORM_FORMAT(G, NV, MODE)                                                  \
+    if (a.format < 0) VA_NORM_BWD(G, NV, MODE, -1);                                  \
+    else if (a.format == VA_ACT8_INT8) VA_NORM_BWD(G, NV, MODE, VA_ACT8_INT8);       \
+    else VA_NORM_BWD(G, NV, MODE, VA_ACT8_E4M3);
+#define VA_NORM_GO(G, NV, FWD, BWD)                          \
+    {                                                        \
+        if (mode == STREAM) { VA_NORM_FORMAT(G, NV, STREAM) } \
+        else if (mode == WIDE) { VA_NORM_FORMAT(G, NV, WIDE) } \
+        else { VA_NORM_FORMAT(G, NV, RAGGED) }               \
+    }
         VA_NORM_SHAPES(VA_NORM_GO)
 #undef VA_NORM_GO
 #undef VA_NORM_FORMAT

@@ -47,26 +47,37 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
 }
 
 // ---- eight channels of a row ----------------------------------------------------------------------------------------
-// WIDE: the eight lie 16-byte aligned and all exist.  Otherwise the first n of them do (0 <= n), each is moved by itself, and the
-// rest read as zero.
-template <bool WIDE>
+// n > 0 of the eight exist; the others read as zero and are not written.  Eight are moved by one 16-byte access (8-byte, of codes),
+// whatever their alignment: the memory system takes one at any address, and the type says so to the compiler.  The rows' shape:
+//   RAGGED  the last run of a row may be shorter than eight, and is moved element by element
+//   WIDE    every run has eight (n >= 8 or n <= 0)
+//   STREAM  and they go past the caches, which will not hold them until they are used again.  For rows of whole 128-byte lines only: where
+//           a line is written by two instructions it pays twice (rotary heads of 64 channels 426 -> 535 us).
+enum RowMode { RAGGED, WIDE, STREAM };
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(1)));
+template <int MODE>
 __device__ __forceinline__ u32x4 load8(const uint16_t* p, int n) {
-    if (WIDE) return n > 0 ? *(const u32x4*)p : u32x4{0, 0, 0, 0};
     u32x4 w = {0, 0, 0, 0};
+    if (MODE != RAGGED ? n > 0 : n >= 8) {
+        w = MODE == STREAM ? __builtin_nontemporal_load((const u32x4_any*)p) : *(const u32x4_any*)p;
+    } else if (MODE == RAGGED && n > 0) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < n) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+        for (int e = 0; e < 7; ++e)
+            if (e < n) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+    }
     return w;
 }
-template <bool WIDE>
+template <int MODE>
 __device__ __forceinline__ void store8(uint16_t* p, const u32x4& w, int n) {
-    if (WIDE) {
-        if (n > 0) *(u32x4*)p = w;
-        return;
-    }
+    if (MODE != RAGGED ? n > 0 : n >= 8) {
+        if (MODE == STREAM) __builtin_nontemporal_store(w, (u32x4_any*)p);
+        else *(u32x4_any*)p = w;
+    } else if (MODE == RAGGED && n > 0) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < n) p[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+        for (int e = 0; e < 7; ++e)
+            if (e < n) p[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+    }
 }
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -125,39 +136,44 @@ __device__ __forceinline__ u32x2 act8_encode(const float* x, float scale, int fo
     }
     return w;
 }
-__device__ __forceinline__ void act8_decode(const u32x2& w, float scale, int format, float* x) {
+// code * scale - off (off = 0: with the one rounding that the format's value has).
+__device__ __forceinline__ void act8_decode(const u32x2& w, float scale, int format, float* x, float off = 0.f) {
     if (format == VA_ACT8_INT8) {
         // code + 128 as an unsigned byte: one conversion, and 128 scale comes off again exactly, with the one rounding of the product
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            x[e] = fmaf((float)(((w[e >> 2] ^ 0x80808080u) >> (8 * (e & 3))) & 255u), scale, -128.f * scale);
+            x[e] = fmaf((float)(((w[e >> 2] ^ 0x80808080u) >> (8 * (e & 3))) & 255u), scale, -128.f * scale - off);
     } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-            x[4 * i] = lo[0] * scale; x[4 * i + 1] = lo[1] * scale;
-            x[4 * i + 2] = hi[0] * scale; x[4 * i + 3] = hi[1] * scale;
+            x[4 * i] = fmaf(lo[0], scale, -off); x[4 * i + 1] = fmaf(lo[1], scale, -off);
+            x[4 * i + 2] = fmaf(hi[0], scale, -off); x[4 * i + 3] = fmaf(hi[1], scale, -off);
         }
     }
 }
-template <bool WIDE>
+template <int MODE>
 __device__ __forceinline__ u32x2 load_codes(const uint8_t* p, int n) {
-    if (WIDE) return n > 0 ? *(const u32x2*)p : u32x2{0, 0};
     u32x2 w = {0, 0};
+    if (MODE != RAGGED ? n > 0 : n >= 8) {
+        w = MODE == STREAM ? __builtin_nontemporal_load((const u32x2_any*)p) : *(const u32x2_any*)p;
+    } else if (MODE == RAGGED && n > 0) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < n) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
+        for (int e = 0; e < 7; ++e)
+            if (e < n) w[e >> 2] |= (uint32_t)p[e] << (8 * (e & 3));
+    }
     return w;
 }
-template <bool WIDE>
+template <int MODE>
 __device__ __forceinline__ void store_codes(uint8_t* p, const u32x2& w, int n) {
-    if (WIDE) {
-        if (n > 0) *(u32x2*)p = w;
-        return;
-    }
+    if (MODE != RAGGED ? n > 0 : n >= 8) {
+        if (MODE == STREAM) __builtin_nontemporal_store(w, (u32x2_any*)p);
+        else *(u32x2_any*)p = w;
+    } else if (MODE == RAGGED && n > 0) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (e < n) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+        for (int e = 0; e < 7; ++e)
+            if (e < n) p[e] = (uint8_t)(w[e >> 2] >> (8 * (e & 3)));
+    }
 }
 
 }  // namespace va

@@ -20,9 +20,10 @@ __device__ __forceinline__ void rotary_angle(int position, float inv_freq, float
 }
 
 template <int VEC> struct RotaryVec;
-template <> struct RotaryVec<8> { typedef u32x4 type; };
-template <> struct RotaryVec<4> { typedef u32x2 type; };
-template <> struct RotaryVec<1> { typedef uint16_t type; };
+// (at any alignment: see load8)
+template <> struct RotaryVec<8> { typedef u32x4 type; typedef u32x4_any any; };
+template <> struct RotaryVec<4> { typedef u32x2 type; typedef u32x2 any __attribute__((aligned(2))); };
+template <> struct RotaryVec<1> { typedef uint16_t type; typedef uint16_t any; };
 
 template <int VEC>
 __device__ __forceinline__ void unpack_vec(const typename RotaryVec<VEC>::type& w, float* x) {
@@ -52,6 +53,7 @@ template <int VEC, bool INTERLEAVED>
 __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
     extern __shared__ float angles[];  // cos [tokens_per_wg][P], then sin
     typedef typename RotaryVec<VEC>::type Vec;
+    typedef typename RotaryVec<VEC>::any VecAny;
     const int P = a.num_pairs, D = a.head_dim;
     const int64_t t0 = (int64_t)blockIdx.x * a.tokens_per_wg;
     const int nt = (int)min((int64_t)a.tokens_per_wg, a.total_tokens - t0);
@@ -98,8 +100,8 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
             src = a.v + (t0 + t) * a.v_stride + (size_t)head * D;
             dst = a.v_out + (t0 + t) * a.v_out_stride + (size_t)head * D;
         }
-        Vec w0 = *(const Vec*)(src + c0), w1 = {};
-        if (two) w1 = *(const Vec*)(src + c1);
+        Vec w0 = *(const VecAny*)(src + c0), w1 = {};
+        if (two) w1 = *(const VecAny*)(src + c1);
         if (turn) {
             float x0[VEC], x1[VEC];
             unpack_vec<VEC>(w0, x0);
@@ -118,8 +120,8 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
             w0 = pack_vec<VEC>(x0);
             w1 = pack_vec<VEC>(x1);
         }
-        *(Vec*)(dst + c0) = w0;
-        if (two) *(Vec*)(dst + c1) = w1;
+        *(VecAny*)(dst + c0) = w0;
+        if (two) *(VecAny*)(dst + c1) = w1;
     }
 }
 
@@ -165,16 +167,8 @@ hipError_t launch_rotary_positions(int total_tokens, int num_segments, int merge
     return hipGetLastError();
 }
 
-// Widest run of channels that every tensor's rows and the pairs allow.
-static int rotary_vec(const RotaryArgs& a) {
-    uint64_t bits = (uint64_t)(uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.k_out | (uintptr_t)a.v_out;
-    bits |= 2 * (uint64_t)(a.q_stride | a.k_stride | a.q_out_stride | a.k_out_stride | a.head_dim | a.num_pairs);
-    if (a.v) bits |= 2 * (uint64_t)(a.v_stride | a.v_out_stride);
-    return bits % 16 == 0 ? 8 : bits % 8 == 0 ? 4 : 1;
-}
-
 hipError_t launch_rotary(RotaryArgs a, hipStream_t stream) {
-    const int vec = rotary_vec(a);
+    const int shape = a.head_dim | a.num_pairs, vec = shape % 8 == 0 ? 8 : shape % 4 == 0 ? 4 : 1;  // the widest run that divides both
     a.tokens_per_wg = a.total_tokens >= 4096 ? (a.num_pairs <= 32 ? 8 : 4) : 1;
     const dim3 grid((unsigned)((a.total_tokens + (int64_t)a.tokens_per_wg - 1) / a.tokens_per_wg)), block(ROT_THREADS);
     const size_t lds = 2 * sizeof(float) * a.tokens_per_wg * a.num_pairs;
