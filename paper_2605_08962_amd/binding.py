@@ -124,7 +124,7 @@ class _PythonHalf:
     def fwd(*args):
         return NotImplemented
 
-    bwd = merge = fwd
+    bwd = merge = positions = rotary = act8_pack = act8_unpack = bwd_act8 = norm_fwd = norm_bwd = fwd
 
 
 def _load_host():
@@ -148,9 +148,13 @@ def _load_host():
                           stacklevel=3)
             host = _PythonHalf
         else:
-            host.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-                lib.varlen_attn_fwd_workspace_bytes, lib.varlen_attn_bwd_workspace_bytes, lib.varlen_attn_fwd, lib.varlen_attn_bwd,
-                lib.varlen_attn_merge)))
+            address = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
+            host.bind(*map(address, (lib.varlen_attn_fwd_workspace_bytes, lib.varlen_attn_bwd_workspace_bytes, lib.varlen_attn_fwd,
+                                     lib.varlen_attn_bwd, lib.varlen_attn_merge)))
+            host.bind_block(*map(address, (lib.varlen_attn_rotary_positions, lib.varlen_attn_rotary_fwd, lib.varlen_attn_rotary_bwd,
+                                           lib.varlen_attn_act8_pack, lib.varlen_attn_act8_unpack,
+                                           lib.varlen_attn_bwd_act8_workspace_bytes, lib.varlen_attn_bwd_act8, lib.varlen_attn_norm_fwd,
+                                           lib.varlen_attn_norm_bwd_workspace_bytes, lib.varlen_attn_norm_bwd)), Act8)
         _host = host
     return _host
 
@@ -405,6 +409,13 @@ _ACT8_OF_TYPE = {torch.int8: 0, torch.float8_e4m3fn: 1}
 _WEIGHT_TYPES = {torch.bfloat16: 0, torch.float32: 1}
 
 
+def _done(answer):
+    """Whether the native half has done the call: an answer that is not NotImplemented, nor a status, which is raised."""
+    if type(answer) is int:
+        _check(answer)
+    return answer is not NotImplemented
+
+
 class _On:
     """Everything a call is given has to be on one GPU, which is made the current one for it."""
 
@@ -463,6 +474,10 @@ def varlen_attn_rotary_positions(cu_rows, grids, total_tokens, first=None, merge
     """Positions int32 [3, total_tokens] (time, height, width) of packed text, images and video; asynchronous on the stream.
     Segment s holds the tokens [cu_rows[s], cu_rows[s + 1]); grids int32 [S, 3] its time, height and width in patches, laid out in blocks of
     merge x merge (height or width 0: text, whose tokens count up on all axes); first int32 [S]: added to a segment's positions."""
+    if stream is None and out is None:
+        answer = (_host or _load_host()).positions(cu_rows, grids, total_tokens, first, merge)
+        if _done(answer):
+            return answer
     for t, n in ((cu_rows, "cu_rows"), (grids, "grids"), (first, "first"), (out, "out")):
         if t is not None:
             _require(t, torch.int32, n)
@@ -480,6 +495,10 @@ def varlen_attn_rotary_positions(cu_rows, grids, total_tokens, first=None, merge
 
 
 def _rotary(inverse, names, q, k, v, positions, inv_freq, pair_axis, interleaved, q_out, k_out, v_out, stream):
+    if stream is None:
+        answer = (_host or _load_host()).rotary(inverse, q, k, v, positions, inv_freq, pair_axis, bool(interleaved), q_out, k_out, v_out)
+        if _done(answer):
+            return answer
     ins, outs = dict(zip(names, (q, k, v))), dict(zip((n + "_out" for n in names), (q_out, k_out, v_out)))
     strides = [0 if t is None else _token_stride(t, n) for n, t in ins.items()]
     if k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
@@ -557,6 +576,10 @@ def varlen_attn_act8_pack(tensors, format="int8", out=None, stream=None):
         raise ValueError("format must be int8 or e4m3")
     number, code_type = _ACT8_FORMATS[format]
     tensors = list(tensors)
+    if stream is None and out is None:
+        answer = (_host or _load_host()).act8_pack(tensors, number)
+        if _done(answer):
+            return answer
     strides = [_token_stride(t, f"tensors[{i}]", (2, 3)) for i, t in enumerate(tensors)]
     if out is not None:
         out = list(out)
@@ -581,6 +604,10 @@ def varlen_attn_act8_unpack(packed, out=None, stream=None):
     """The bf16 tensors that a list of Act8 stands for; asynchronous on the stream.
     out: the caller's own tensors of the same shapes, contiguous or parts of wider ones."""
     packed = list(packed)
+    if stream is None and out is None:
+        answer = (_host or _load_host()).act8_unpack(packed)
+        if _done(answer):
+            return answer
     formats = [_check_act8(x, f"packed[{i}]") for i, x in enumerate(packed)]
     if len(set(formats)) > 1:
         raise ValueError("packed must be of one format")
@@ -611,6 +638,11 @@ def bwd_act8_workspace_bytes(params):
 def varlen_attn_bwd_act8(dout, q, k, v, out, lse, cu_seqlens, causal, softmax_scale, dq=None, dk=None, dv=None, workspace=None,
                          stream=None, max_seqlen=0, kv_splits=0):
     """varlen_attn_bwd with q, k, v and out in 8 bits (Act8s of one format, from varlen_attn_act8_pack); the other arguments as there."""
+    if stream is None:
+        answer = (_host or _load_host()).bwd_act8(dout, q, k, v, out, lse, cu_seqlens, bool(causal), float(softmax_scale), dq, dk, dv,
+                                                  workspace, int(kv_splits), int(max_seqlen))
+        if _done(answer):
+            return answer
     _require(dout, torch.bfloat16, "dout")
     formats = {_check_act8(x, n) for x, n in ((q, "q"), (k, "k"), (v, "v"), (out, "out"))}
     if len(formats) > 1:
@@ -670,11 +702,15 @@ def varlen_attn_norm_fwd(x, weight=None, bias=None, eps=1e-5, residual=None, sav
     weight, bias: bf16 or fp32 [C], or None.  residual: contiguous, x's shape; the norm is then of summed = bf16(x + residual).
     save: "int8" or "e4m3": what is normed is left in 8 bits too (saved, an Act8), for varlen_attn_norm_bwd.
     out: the caller's own contiguous tensor of x's shape."""
-    stride = _token_stride(x, "x", (2, 3))
-    shape = x.shape
     if save is not None and save not in _ACT8_FORMATS:
         raise ValueError("save must be int8 or e4m3")
     number, code_type = _ACT8_FORMATS[save or "int8"]
+    if stream is None:
+        answer = (_host or _load_host()).norm_fwd(x, weight, bias, float(eps), residual, number if save else None, out)
+        if _done(answer):
+            return NormForward._make(answer)
+    stride = _token_stride(x, "x", (2, 3))
+    shape = x.shape
     _contiguous_like(residual, shape, "residual")
     _contiguous_like(out, shape, "out")
     p = _norm_params(shape, _check_weights(weight, bias, shape[-1]), number, eps, x_stride=stride)
@@ -698,6 +734,10 @@ def varlen_attn_norm_bwd(dy, x, mean, rstd, weight=None, dsummed=None, dx=None, 
     x: what was normed: the forward's x, its summed where it had a residual, or its saved Act8.  mean, rstd: the forward's.
     dsummed: the gradient that reaches summed on its own way, added to dx (which is the gradient of x and of residual).
     dy, x and dx may be parts of wider tensors; dx, workspace: the caller's own."""
+    if stream is None and workspace is None:
+        answer = (_host or _load_host()).norm_bwd(dy, x, mean, rstd, weight, dsummed, dx)
+        if _done(answer):
+            return answer
     dy_stride = _token_stride(dy, "dy", (2, 3))
     shape, packed = dy.shape, isinstance(x, Act8)
     number = _check_act8(x, "x") if packed else 0

@@ -11,7 +11,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libvarlen_attn.so")
-HOST_SOURCES = [os.path.join(CSRC, "va_host.cpp"), os.path.join(HERE, "..", "include", "varlen_attn.h")]
+HOST_SOURCES = [os.path.join(CSRC, "va_host.cpp"), os.path.join(CSRC, "va_host_block.h"),
+                os.path.join(HERE, "..", "include", "varlen_attn.h")]
 # (source, object name, extra flags).  va_bwd.hip is built in parts, each under the instruction-scheduling strategy that
 # measured best for its kernels among the default, iterative-ilp, iterative-minreg, iterative-maxocc, max-ilp and
 # max-memory-clause (64 ViT samples, 16 heads, unless said otherwise; the forward does best with the default):

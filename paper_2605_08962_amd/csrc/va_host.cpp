@@ -1,5 +1,5 @@
-// The Python binding's usual call in native code: what binding.py's varlen_attn_fwd, varlen_attn_bwd and varlen_attn_merge do
-// between being called and calling the library, for plain tensors that pass every check.  Anything else (a check that fails, a tensor
+// The Python binding's usual call in native code: what binding.py's varlen_attn_fwd, varlen_attn_bwd and varlen_attn_merge (and the
+// operators around attention, va_host_block.h) do between being called and calling the library, for plain tensors that pass every check.  Anything else (a check that fails, a tensor
 // subclass, a torch function mode, allocations for another stream) gets NotImplemented, and binding.py goes through its own
 // checks, which name the fault.
 //
@@ -9,9 +9,12 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <initializer_list>
 
 #include "../../include/varlen_attn.h"
 
@@ -240,7 +243,14 @@ PyObject* merge(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-PyMethodDef methods[] = {{"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, nullptr},
+#include "va_host_block.h"
+
+#define VA_HOST_METHOD(NAME, F) {NAME, (PyCFunction)(void (*)())F, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {VA_HOST_METHOD("bind_block", bind_block), VA_HOST_METHOD("positions", rotary_positions),
+                         VA_HOST_METHOD("rotary", rotary), VA_HOST_METHOD("act8_pack", act8_pack),
+                         VA_HOST_METHOD("act8_unpack", act8_unpack), VA_HOST_METHOD("bwd_act8", bwd_act8),
+                         VA_HOST_METHOD("norm_fwd", norm_fwd), VA_HOST_METHOD("norm_bwd", norm_bwd),
+                         {"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, nullptr},
                          {"fwd", (PyCFunction)(void (*)())fwd, METH_FASTCALL, nullptr},
                          {"bwd", (PyCFunction)(void (*)())bwd, METH_FASTCALL, nullptr},
                          {"merge", (PyCFunction)(void (*)())merge, METH_FASTCALL, nullptr},
