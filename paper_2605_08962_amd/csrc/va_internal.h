@@ -151,7 +151,10 @@ struct RotaryArgs {
     const int32_t* pair_axis;  // [num_pairs]
     int total_tokens, num_q_heads, num_kv_heads, head_dim, num_pairs, num_axes;
     bool interleaved, inverse;
-    int tokens_per_wg;  // (filled by the launch)
+    // (filled by the launch)
+    struct Divisor { uint32_t factor, shift; } by_token, by_head, by_v, by_pairs;
+    int per_token, per_head, per_v;  // items of a token, a head of q or k, a head of v
+    int tile, tile_tokens;           // items and tokens of a workgroup
 };
 hipError_t launch_rotary(RotaryArgs a, hipStream_t stream);
 hipError_t launch_rotary_positions(int total_tokens, int num_segments, int merge, const int32_t* cu, const int32_t* grids,

@@ -75,15 +75,8 @@ struct Weights {
     }
 };
 
-// Where row `row` of a tensor with a stride between tokens starts.
 __device__ __forceinline__ int64_t row_offset(const NormArgs& a, int64_t row, int64_t stride) {
-    if (stride == (int64_t)a.rows_per_token * a.channels) return row * a.channels;
-    if (a.rows_per_token == 1) return row * stride;
-    if (a.rows <= INT32_MAX) {  // (a division in 64 bits is 100 instructions, on rows of as few as 8 channels a lane)
-        const uint32_t r = (uint32_t)row, t = r / (uint32_t)a.rows_per_token;
-        return t * stride + (int64_t)(r - t * (uint32_t)a.rows_per_token) * a.channels;
-    }
-    return row / a.rows_per_token * stride + row % a.rows_per_token * a.channels;
+    return strided_row(row, a.rows, a.rows_per_token, a.channels, stride);
 }
 
 template <int G, int NV, int MODE>

@@ -20,9 +20,7 @@ __device__ __forceinline__ void rotary_angle(int position, float inv_freq, float
 }
 
 template <int VEC> struct RotaryVec;
-// (at any alignment: see load8)
-template <> struct RotaryVec<8> { typedef u32x4 type; typedef u32x4_any any; };
-template <> struct RotaryVec<4> { typedef u32x2 type; typedef u32x2 any __attribute__((aligned(2))); };
+template <> struct RotaryVec<4> { typedef u32x2 type; typedef u32x2 any __attribute__((aligned(2))); };  // (at any alignment: see load8)
 template <> struct RotaryVec<1> { typedef uint16_t type; typedef uint16_t any; };
 
 template <int VEC>
@@ -47,81 +45,222 @@ __device__ __forceinline__ typename RotaryVec<VEC>::type pack_vec(const float* x
     return w;
 }
 
-// One workgroup turns a.tokens_per_wg tokens.  A thread's item is two runs of VEC channels: of the two halves of VEC pairs, or
-// (copied channels and v) side by side.  Both are read before either is written, so a tensor may be turned in place.
+// n / d for n < 2^31 by a product.
+__device__ __forceinline__ uint32_t divide(uint32_t n, RotaryArgs::Divisor d) { return (uint32_t)(((uint64_t)n * d.factor) >> d.shift); }
+
+// Heads or numbers of pairs that whole 16-byte runs do not divide.  One workgroup turns a.tile_tokens tokens.  A thread's item is two runs
+// of VEC channels: of the two halves of VEC pairs, or (copied channels and v) side by side.  Both are read before either is written,
+// so a tensor may be turned in place.  Two items are under way together, the first of them while the angles are formed.
 template <int VEC, bool INTERLEAVED>
 __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
-    extern __shared__ float angles[];  // cos [tokens_per_wg][P], then sin
+    constexpr int U = 2;
+    extern __shared__ float angles[];  // cos [tile_tokens][P], then sin
     typedef typename RotaryVec<VEC>::type Vec;
     typedef typename RotaryVec<VEC>::any VecAny;
     const int P = a.num_pairs, D = a.head_dim;
-    const int64_t t0 = (int64_t)blockIdx.x * a.tokens_per_wg;
-    const int nt = (int)min((int64_t)a.tokens_per_wg, a.total_tokens - t0);
+    const int64_t t0 = (int64_t)blockIdx.x * a.tile_tokens;
+    const int nt = (int)min((int64_t)a.tile_tokens, a.total_tokens - t0);
+    const int turned = P / VEC;                     // items of a head that turn; then those that are copied
+    const int nq = a.num_q_heads * a.per_head, nqk = nq + a.num_kv_heads * a.per_head;
+    const int items = nt * a.per_token;
+
+    struct Item {
+        uint16_t *d0, *d1;  // null: nothing there
+        Vec w0, w1;
+        int angle;          // of the first pair in LDS; below 0: copied
+    } it[U];
+    auto fetch = [&](int i, Item& x) {
+        x.d0 = x.d1 = nullptr;
+        if (i >= items) return;
+        const int t = (int)divide(i, a.by_token);
+        int r = i - t * a.per_token;
+        const uint16_t* src;
+        uint16_t* dst;
+        int c0, c1;
+        x.angle = -1;
+        if (r < nqk) {
+            const bool is_k = r >= nq;
+            r -= is_k ? nq : 0;
+            const int head = (int)divide(r, a.by_head), slot = r - head * a.per_head;
+            src = (is_k ? a.k + (t0 + t) * a.k_stride : a.q + (t0 + t) * a.q_stride) + head * D;
+            dst = (is_k ? a.k_out + (t0 + t) * a.k_out_stride : a.q_out + (t0 + t) * a.q_out_stride) + head * D;
+            const bool turn = slot < turned;
+            c0 = turn ? (INTERLEAVED ? 2 * VEC * slot : VEC * slot) : 2 * P + 2 * VEC * (slot - turned);
+            c1 = turn && !INTERLEAVED ? c0 + P : c0 + VEC;
+            if (turn) x.angle = t * P + VEC * slot;
+        } else {
+            r -= nqk;
+            const int head = (int)divide(r, a.by_v);
+            c0 = 2 * VEC * (r - head * a.per_v);
+            c1 = c0 + VEC;
+            src = a.v + (t0 + t) * a.v_stride + head * D;
+            dst = a.v_out + (t0 + t) * a.v_out_stride + head * D;
+        }
+        x.d0 = dst + c0;
+        x.w0 = *(const VecAny*)(src + c0);
+        if (c1 < D) {
+            x.d1 = dst + c1;
+            x.w1 = *(const VecAny*)(src + c1);
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) fetch(threadIdx.x + u * ROT_THREADS, it[u]);
+
     float* const cs = angles;
-    float* const sn = angles + a.tokens_per_wg * P;
+    float* const sn = angles + a.tile_tokens * P;
     for (int i = threadIdx.x; i < nt * P; i += ROT_THREADS) {
-        const int t = i / P, j = i % P;
+        const int t = (int)divide(i, a.by_pairs), j = i - t * P;
         const int axis = min(max(a.pair_axis[j], 0), a.num_axes - 1);
         float c, s;
         rotary_angle(a.positions[(size_t)axis * a.total_tokens + t0 + t], a.inv_freq[j], c, s);
         cs[i] = c;
         sn[i] = a.inverse ? -s : s;
     }
-    __syncthreads();
+    wg_barrier();
 
-    const int turned = P / VEC, copied = ((D - 2 * P) / VEC + 1) / 2;  // items of a head of q or k
-    const int per_head = turned + copied, per_v = (D / VEC + 1) / 2;
-    const int nq = a.num_q_heads * per_head, nk = a.num_kv_heads * per_head, nv = a.v ? a.num_kv_heads * per_v : 0;
-    const int per_token = nq + nk + nv;
-    for (int i = threadIdx.x; i < nt * per_token; i += ROT_THREADS) {
-        const int t = i / per_token;
-        int r = i % per_token;
-        const uint16_t* src;
-        uint16_t* dst;
-        int c0, c1;
-        bool two = true, turn = false;
-        if (r < nq + nk) {
-            const bool is_k = r >= nq;
-            r -= is_k ? nq : 0;
-            const int head = r / per_head, slot = r % per_head;
-            src = (is_k ? a.k + (t0 + t) * a.k_stride : a.q + (t0 + t) * a.q_stride) + (size_t)head * D;
-            dst = (is_k ? a.k_out + (t0 + t) * a.k_out_stride : a.q_out + (t0 + t) * a.q_out_stride) + (size_t)head * D;
-            turn = slot < turned;
-            c0 = turn ? (INTERLEAVED ? 2 * VEC * slot : VEC * slot) : 2 * P + 2 * VEC * (slot - turned);
-            c1 = turn && !INTERLEAVED ? c0 + P : c0 + VEC;
-            two = c1 < D;
-            r = slot;
-        } else {
-            r -= nq + nk;
-            const int head = r / per_v;
-            c0 = 2 * VEC * (r % per_v);
-            c1 = c0 + VEC;
-            two = c1 < D;
-            src = a.v + (t0 + t) * a.v_stride + (size_t)head * D;
-            dst = a.v_out + (t0 + t) * a.v_out_stride + (size_t)head * D;
-        }
-        Vec w0 = *(const VecAny*)(src + c0), w1 = {};
-        if (two) w1 = *(const VecAny*)(src + c1);
-        if (turn) {
-            float x0[VEC], x1[VEC];
-            unpack_vec<VEC>(w0, x0);
-            unpack_vec<VEC>(w1, x1);
-            const float* const c = cs + t * P + VEC * r;
-            const float* const s = sn + t * P + VEC * r;
+    for (int i = threadIdx.x; i < items; i += U * ROT_THREADS) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                // interleaved: the 2 VEC channels side by side hold the pairs (2e, 2e + 1)
-                float& u = INTERLEAVED ? (2 * e < VEC ? x0[2 * e % VEC] : x1[2 * e % VEC]) : x0[e];
-                float& v = INTERLEAVED ? (2 * e + 1 < VEC ? x0[(2 * e + 1) % VEC] : x1[(2 * e + 1) % VEC]) : x1[e];
-                const float u1 = u * c[e] - v * s[e];
-                v = v * c[e] + u * s[e];
-                u = u1;
+        for (int u = 0; u < U; ++u) {
+            Item& x = it[u];
+            if (x.d0 && x.angle >= 0) {
+                float x0[VEC], x1[VEC];
+                unpack_vec<VEC>(x.w0, x0);
+                unpack_vec<VEC>(x.w1, x1);
+                const float* const c = cs + x.angle;
+                const float* const s = sn + x.angle;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    // interleaved: the 2 VEC channels side by side hold the pairs (2e, 2e + 1)
+                    float& p = INTERLEAVED ? (2 * e < VEC ? x0[2 * e % VEC] : x1[2 * e % VEC]) : x0[e];
+                    float& q = INTERLEAVED ? (2 * e + 1 < VEC ? x0[(2 * e + 1) % VEC] : x1[(2 * e + 1) % VEC]) : x1[e];
+                    const float p1 = p * c[e] - q * s[e];
+                    q = q * c[e] + p * s[e];
+                    p = p1;
+                }
+                x.w0 = pack_vec<VEC>(x0);
+                x.w1 = pack_vec<VEC>(x1);
             }
-            w0 = pack_vec<VEC>(x0);
-            w1 = pack_vec<VEC>(x1);
+            if (x.d0) *(VecAny*)x.d0 = x.w0;
+            if (x.d1) *(VecAny*)x.d1 = x.w1;
         }
-        *(VecAny*)(dst + c0) = w0;
-        if (two) *(VecAny*)(dst + c1) = w1;
+#pragma unroll
+        for (int u = 0; u < U; ++u) fetch(i + (U + u) * ROT_THREADS, it[u]);
+    }
+}
+
+template <bool STREAMED>
+__device__ __forceinline__ u32x4 load_run(const uint16_t* p) {
+    return STREAMED ? __builtin_nontemporal_load((const u32x4_any*)p) : *(const u32x4_any*)p;
+}
+// What lane l ^ N holds, N = 4 or 8.
+template <int N>
+__device__ __forceinline__ u32x4 from_lane_xor(const u32x4& w, bool upper) {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (N == 8) r[i] = dpp<0x128>(w[i]);                              // rotated by 8 within 16 lanes
+        else { const uint32_t up = dpp<0x104>(w[i]), down = dpp<0x114>(w[i]); r[i] = upper ? down : up; }  // shifted by 4, either way
+    }
+    return r;
+}
+
+// Heads of whole 16-byte runs.  The runs of a token's heads of q, k and v are numbered in a row, and a workgroup takes a tile of them,
+// whole heads, three a thread: neighbouring threads read and write neighbouring 16 bytes, so that whole lines leave a wave at once
+// (written by two instructions, half a line each, past the caches, they cost up to twice the time).  All of a tile is read before any of
+// it is written.  Where a run's pairs' other channels are:
+//   HERE      in the run itself (interleaved)        LANE4, LANE8   4 or 8 lanes on (whole heads of 64 and 128 channels)
+//   MEMORY    elsewhere: read once more, out of the line that another thread of the tile has just fetched
+// STREAMED: past the caches.  Measured, TB/s forward, one / two / three / four runs a thread, through the caches and past them (and all
+// loads of the pair, halves written by one thread: 5.25, 5.2, 4.9, 4.8 at best)
+//   178572 x 16/16 heads of 64   5.80 5.90 5.68 5.53 / 5.46 6.05 6.03 6.01       32768 x 32/8 of 128   5.54 5.60 5.55 5.53 / 5.56 5.89 6.02 6.12
+//   100000 x 16/16 of 80         4.55 5.40 5.41 4.99 / 4.58 5.03 5.82 5.10       ... interleaved       5.71 5.56 5.54 5.39 / 5.48 6.00 6.09 5.96
+enum RotaryPartner { HERE, LANE4, LANE8, MEMORY };
+constexpr int ROT_RUNS = 3;
+template <int PARTNER, bool STREAMED>
+__global__ void __launch_bounds__(ROT_THREADS) rotary_flat_kernel(RotaryArgs a) {
+    constexpr int U = ROT_RUNS;
+    constexpr bool INTERLEAVED = PARTNER == HERE;
+    extern __shared__ float angles[];  // cos [tile_tokens][P], then sin
+    const int P = a.num_pairs;
+    const int64_t f0 = (int64_t)blockIdx.x * a.tile, total = (int64_t)a.total_tokens * a.per_token;
+    const int64_t t0 = f0 / a.per_token;
+    const int r0 = (int)(f0 - t0 * a.per_token), n = (int)min((int64_t)a.tile, total - f0);
+    const int nq = a.num_q_heads * a.per_head, nqk = nq + a.num_kv_heads * a.per_head;
+    u32x4 w[U], m[U];
+    uint16_t* dst[U];
+    int angle[U];  // of the run's first pair in LDS; below 0: copied
+    bool second[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = threadIdx.x + u * ROT_THREADS;
+        dst[u] = nullptr;
+        angle[u] = -1;
+        second[u] = false;
+        if (i >= n) continue;
+        const int x = r0 + i, t = (int)divide(x, a.by_token), r = x - t * a.per_token;
+        const int64_t token = t0 + t;
+        const uint16_t* src;
+        if (r < nqk) {
+            const bool is_k = r >= nq;
+            src = (is_k ? a.k + token * a.k_stride : a.q + token * a.q_stride) + 8 * (r - (is_k ? nq : 0));
+            dst[u] = (is_k ? a.k_out + token * a.k_out_stride : a.q_out + token * a.q_out_stride) + 8 * (r - (is_k ? nq : 0));
+            const int c = 8 * (r - (int)divide(r, a.by_head) * a.per_head);  // first channel in the head
+            if (c < 2 * P) {
+                if (INTERLEAVED) {
+                    angle[u] = t * P + c / 2;
+                } else {
+                    second[u] = c >= P;
+                    angle[u] = t * P + c - (second[u] ? P : 0);
+                    if (PARTNER == MEMORY) m[u] = load_run<STREAMED>(src + (second[u] ? -P : P));
+                }
+            }
+        } else {
+            src = a.v + token * a.v_stride + 8 * (r - nqk);
+            dst[u] = a.v_out + token * a.v_out_stride + 8 * (r - nqk);
+        }
+        w[u] = load_run<STREAMED>(src);
+    }
+
+    const int tokens = (int)divide(r0 + n - 1, a.by_token) + 1;
+    float* const cs = angles;
+    float* const sn = angles + a.tile_tokens * P;
+    for (int i = threadIdx.x; i < tokens * P; i += ROT_THREADS) {
+        const int t = (int)divide(i, a.by_pairs), j = i - t * P;
+        const int axis = min(max(a.pair_axis[j], 0), a.num_axes - 1);
+        float c, s;
+        rotary_angle(a.positions[(size_t)axis * a.total_tokens + t0 + t], a.inv_freq[j], c, s);
+        cs[i] = c;
+        sn[i] = a.inverse ? -s : s;
+    }
+    wait_vmcnt<0>();  // (a partner may be written by another thread, where the tensor is turned in place)
+    wg_barrier();
+
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (PARTNER == LANE4 || PARTNER == LANE8) m[u] = from_lane_xor<PARTNER == LANE8 ? 8 : 4>(w[u], second[u]);  // (all lanes)
+        if (!dst[u]) continue;
+        if (angle[u] >= 0) {
+            float x[8], y[8];
+            to_float8(w[u], x);
+            const float* const c = cs + angle[u];
+            const float* const s = sn + angle[u];
+            if (INTERLEAVED) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[2 * e] = x[2 * e] * c[e] - x[2 * e + 1] * s[e];
+                    y[2 * e + 1] = x[2 * e + 1] * c[e] + x[2 * e] * s[e];
+                }
+            } else {
+                float p[8];
+                to_float8(m[u], p);
+                const float sign = second[u] ? 1.f : -1.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = x[e] * c[e] + p[e] * (sign * s[e]);
+            }
+            w[u] = to_bf16x8(y);
+        }
+        if (STREAMED) __builtin_nontemporal_store(w[u], (u32x4_any*)dst[u]);
+        else *(u32x4_any*)dst[u] = w[u];
     }
 }
 
@@ -167,18 +306,57 @@ hipError_t launch_rotary_positions(int total_tokens, int num_segments, int merge
     return hipGetLastError();
 }
 
+static RotaryArgs::Divisor divisor(uint32_t d) {
+    uint32_t l = 0;  // the smallest with 2^l >= d; then ceil(2^(31 + l) / d) < 2^32 is exact for n < 2^31
+    while (((uint64_t)1 << l) < d) ++l;
+    return {(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), 31 + l};
+}
+
 hipError_t launch_rotary(RotaryArgs a, hipStream_t stream) {
-    const int shape = a.head_dim | a.num_pairs, vec = shape % 8 == 0 ? 8 : shape % 4 == 0 ? 4 : 1;  // the widest run that divides both
-    a.tokens_per_wg = a.total_tokens >= 4096 ? (a.num_pairs <= 32 ? 8 : 4) : 1;
-    const dim3 grid((unsigned)((a.total_tokens + (int64_t)a.tokens_per_wg - 1) / a.tokens_per_wg)), block(ROT_THREADS);
-    const size_t lds = 2 * sizeof(float) * a.tokens_per_wg * a.num_pairs;
-#define VA_ROTARY(VEC, INTER) hipLaunchKernelGGL((rotary_kernel<VEC, INTER>), grid, block, lds, stream, a)
-#define VA_ROTARY_STYLE(VEC) if (a.interleaved) VA_ROTARY(VEC, true); else VA_ROTARY(VEC, false)
-    if (vec == 8) { VA_ROTARY_STYLE(8); }
-    else if (vec == 4) { VA_ROTARY_STYLE(4); }
-    else { VA_ROTARY_STYLE(1); }
-#undef VA_ROTARY_STYLE
+    const dim3 block(ROT_THREADS);
+    const int kinds = a.v ? 2 : 1;
+    a.by_pairs = divisor(a.num_pairs);
+    if (a.head_dim % 8 == 0 && a.num_pairs % (a.interleaved ? 4 : 8) == 0) {
+        a.per_head = a.head_dim / 8;
+        a.per_token = (a.num_q_heads + kinds * a.num_kv_heads) * a.per_head;
+        a.tile = ROT_THREADS * ROT_RUNS / a.per_head * a.per_head;
+        a.tile_tokens = a.tile / a.per_token + 2;
+        a.by_token = divisor(a.per_token);
+        a.by_head = divisor(a.per_head);
+        const int64_t runs = (int64_t)a.total_tokens * a.per_token, wgs = (runs + a.tile - 1) / a.tile;
+        if (wgs > INT32_MAX) return hipErrorInvalidConfiguration;
+        const dim3 grid((unsigned)wgs);
+        const size_t lds = 2 * sizeof(float) * a.tile_tokens * a.num_pairs;
+        const bool streamed = runs * 32 > (int64_t)256 << 20;  // beyond the last-level cache nothing is found there again
+        const bool whole = a.head_dim == 2 * a.num_pairs;
+        const int partner = a.interleaved ? HERE : whole && a.num_pairs == 32 ? LANE4 : whole && a.num_pairs == 64 ? LANE8 : MEMORY;
+#define VA_ROTARY(PARTNER)                                                                                               \
+    if (streamed) hipLaunchKernelGGL((rotary_flat_kernel<PARTNER, true>), grid, block, lds, stream, a);                  \
+    else hipLaunchKernelGGL((rotary_flat_kernel<PARTNER, false>), grid, block, lds, stream, a);                          \
+    break;
+        switch (partner) {
+            case HERE: VA_ROTARY(HERE)
+            case LANE4: VA_ROTARY(LANE4)
+            case LANE8: VA_ROTARY(LANE8)
+            default: VA_ROTARY(MEMORY)
+        }
 #undef VA_ROTARY
+        return hipGetLastError();
+    }
+    const int vec = (a.head_dim | a.num_pairs) % 4 == 0 ? 4 : 1;  // the widest run that divides both
+    a.tile_tokens = a.total_tokens >= 4096 ? 4 : 1;
+    a.per_head = a.num_pairs / vec + ((a.head_dim - 2 * a.num_pairs) / vec + 1) / 2;
+    a.per_v = (a.head_dim / vec + 1) / 2;
+    a.per_token = (a.num_q_heads + a.num_kv_heads) * a.per_head + (a.v ? a.num_kv_heads * a.per_v : 0);
+    a.by_token = divisor(a.per_token);
+    a.by_head = divisor(a.per_head);
+    a.by_v = divisor(a.per_v);
+    const dim3 grid((unsigned)((a.total_tokens + (int64_t)a.tile_tokens - 1) / a.tile_tokens));
+    const size_t lds = 2 * sizeof(float) * a.tile_tokens * a.num_pairs;
+    if (vec == 4 && a.interleaved) hipLaunchKernelGGL((rotary_kernel<4, true>), grid, block, lds, stream, a);
+    else if (vec == 4) hipLaunchKernelGGL((rotary_kernel<4, false>), grid, block, lds, stream, a);
+    else if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<1, true>), grid, block, lds, stream, a);
+    else hipLaunchKernelGGL((rotary_kernel<1, false>), grid, block, lds, stream, a);
     return hipGetLastError();
 }
 
