@@ -20,6 +20,8 @@ struct RowGroup {
     static constexpr int ROWS = THREADS / G;        // rows a workgroup has in work at a time
     static constexpr int WAVES = G > 64 ? G / 64 : 1;
     static constexpr int LANES = G > 64 ? 64 : G;
+    // Which of the workgroup's rows this thread works on.  Where a whole wave shares it, a scalar: then a row's addresses are, too.
+    __device__ __forceinline__ static int row_in_wg() { return G >= 64 ? uniform_wave_id() / WAVES : (int)threadIdx.x / G; }
 };
 
 // Sums of N values over the threads of a row.  `at` alternates between the two halves of `lds`, so that one barrier a sum is enough.
@@ -98,7 +100,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
             if (a.residual) rs[j] = load8<MODE>((const uint16_t*)a.residual + row * C + col, n);
         }
     };
-    int64_t row = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / G;
+    int64_t row = (int64_t)blockIdx.x * R::ROWS + R::row_in_wg();
     fetch(row);
     weight.template fill<MODE>(a.weight, a.weight_type, C, 1.f);
     bias.template fill<MODE>(a.bias, a.weight_type, C, 0.f);
@@ -124,7 +126,8 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
             if (a.format >= 0) {
                 constexpr int L = R::LANES < 16 ? R::LANES : 16;
                 const float s = act8_scale(lanes_max<L>(magnitude8(kept)), a.format);
-                store_codes<MODE>((uint8_t*)a.codes + row * C + col, act8_encode(h[j], s, a.format), n);
+                // (through the caches: 8 bytes a thread are half a line a wave at the row's end; 5.07 -> 5.36 TB/s at 1280 channels)
+                store_codes<MODE == STREAM ? WIDE : MODE>((uint8_t*)a.codes + row * C + col, act8_encode(h[j], s, a.format), n);
                 if (lane % L == 0 && n > 0) a.scales[row * blocks + col / kAct8Block] = s;
             }
 #pragma unroll
@@ -202,7 +205,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
             next.dy[j] = load8<MODE>(dy + col, n);
         }
     };
-    int64_t row = (int64_t)blockIdx.x * R::ROWS + threadIdx.x / G;
+    int64_t row = (int64_t)blockIdx.x * R::ROWS + R::row_in_wg();
     fetch(row);
     u.weight.template fill<MODE>(a.weight, a.weight_type, C, 1.f);
     __syncthreads();
@@ -327,14 +330,18 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* __restrict_
 }
 
 // Threads a row, runs a thread, workgroups a CU forward and backward.  Rows of up to 2048 channels stay in one wave, whose sums need
-// no barrier.  Two workgroups a CU that read ahead are more than the memory needs where rows are long, and more of them are slower:
-// forward / backward TB/s with 1, 2, 3, 4, 8 a CU, streaming,
-//   178572 x 1024   3.90 5.83 5.61 5.42 5.27 / 3.79 5.81 5.58 5.03 5.45        65537 x 1280   4.04 5.61 5.34 5.37 5.44 / 3.60 5.42 4.35 5.02 4.54
-//   32768 x 32 heads of 128   2.32 3.88 5.10 5.49 4.71 / 2.54 4.35 5.31 5.37 5.33        16000 x 8000   4.50 5.56 4.76 5.30 4.90 / 5.22 4.75 4.31 3.95 2.97
+// no barrier.  Two workgroups a CU that read ahead are what the memory wants where rows are long, and more of them are slower: forward /
+// backward TB/s with 1, 2, 3, 4, 8 a CU,
+//   178572 x 1024   3.92 5.84 5.68 5.47 5.49 / 4.02 6.01 5.67 5.05 5.48        65537 x 1280   3.99 5.63 5.45 5.45 5.33 / 3.76 5.43 4.38 5.02 4.50
+//   65536 x 2048    5.39 5.98 5.69 5.76 5.84 / 4.80 5.71 5.06 5.49 5.12        32768 x 4096   3.52 5.80 5.94 5.54 5.49 / 3.32 5.27 5.31 4.42 4.46
+//   32768 x 32 heads of 128   2.32 3.88 5.13 5.58 4.73 / 2.61 4.47 5.43 5.45 5.38        16000 x 8000   4.46 5.60 4.76 5.33 4.93 / 5.27 4.96 4.54 4.26 3.40
+//   8000 x 16000    5.60 5.37 5.17 4.90 4.15 / 4.95 4.21 3.71 3.32 2.27
+// (the backward's registers allow two at 1280 channels: with three the third waits).  A forward that leaves codes has more to do between
+// a row's arrival and its end, and takes one more: 65537 x 1280 5.36 -> 5.63, 65536 x 2048 5.80 -> 6.30 (two runs a thread: 6.24 -> 5.81).
 #define VA_NORM_SHAPES(GO) \
     if (C <= 64) GO(8, 1, 4, 4) else if (C <= 128) GO(16, 1, 4, 4) else if (C <= 256) GO(32, 1, 4, 4) else if (C <= 512) GO(64, 1, 4, 4) \
     else if (C <= 1024) GO(64, 2, 2, 2) else if (C <= 1536) GO(64, 3, 2, 2) else if (C <= 2048) GO(64, 4, 2, 2) \
-    else if (C <= 4096) GO(256, 2, 2, 2) else if (C <= 8192) GO(256, 4, 2, 1) else GO(1024, 2, 1, 1)
+    else if (C <= 4096) GO(256, 2, 2, 2) else if (C <= 8192) GO(256, 4, 2, 1) else GO(512, 4, 1, 1)
 constexpr int CUS = 256;
 
 // Workgroups: as many as that, with two rows a thread group as soon as every CU has one.
@@ -361,7 +368,7 @@ hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) {
 #define VA_NORM_FWD(G, NV, MODE) hipLaunchKernelGGL((norm_fwd_kernel<G, NV, MODE>), grid, dim3(RowGroup<G>::THREADS), 0, stream, a)
 #define VA_NORM_GO(G, NV, FWD, BWD)                                             \
     {                                                                           \
-        const dim3 grid((unsigned)norm_wgs(a.rows, RowGroup<G>::ROWS, FWD));    \
+        const dim3 grid((unsigned)norm_wgs(a.rows, RowGroup<G>::ROWS, FWD + (NV > 2 && a.format >= 0))); \
         if (mode == STREAM) VA_NORM_FWD(G, NV, STREAM);                         \
         else if (mode == WIDE) VA_NORM_FWD(G, NV, WIDE);                        \
         else VA_NORM_FWD(G, NV, RAGGED);                                        \
