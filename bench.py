@@ -477,6 +477,117 @@ def measure(args, torch, binding, to_gpu_bf16, w, with_bwd, steps, warmup, settl
     return res
 
 
+def block_positions(torch, binding, w, merge=2):
+    """Positions and their table for a workload: height and width of the ViT batch's images, one axis for text."""
+    if w.name.startswith("vit"):
+        rng = np.random.Generator(np.random.PCG64(w.seed))
+        kh, kw = rng.integers(8, 49, size=w.num_seqs), rng.integers(8, 49, size=w.num_seqs)  # (as the lengths were drawn)
+        grids = np.stack([np.ones_like(kh), 2 * kh, 2 * kw], axis=1)
+        assert (grids.prod(axis=1) == w.lengths).all()
+    else:
+        grids = np.zeros((w.num_seqs, 3))
+    cu = torch.from_numpy(w.cu_seqlens).cuda()
+    pairs = w.head_dim // 2
+    half = pairs // 2
+    axis = torch.tensor([1] * half + [2] * (pairs - half), dtype=torch.int32, device="cuda")
+    at = torch.cat([torch.arange(half) / half, torch.arange(pairs - half) / (pairs - half)])
+    pos = binding.varlen_attn_rotary_positions(cu, torch.from_numpy(grids.astype(np.int32)).cuda(), w.total_tokens, merge=merge)
+    return cu, (pos, (10000.0 ** -at).float().cuda(), axis)
+
+
+def block_forward(torch, binding, p, x, residual, cu, turn, causal, scale, max_seqlen, save, mark=lambda name: None):
+    """The attention half of a pre-norm block: the stream x + residual, and what its attention adds to it.  p: norm's weight and bias,
+    the fused projection w_qkv [(Hq + 2 Hkv) D, C] and the output projection w_out [C, Hq D].  save: what the backward keeps of the
+    norm's input and of q, k, v, o: "int8", "e4m3" or None (bf16)."""
+    hq, hkv = p["heads"]
+    f = binding.varlen_attn_norm_fwd(x, p["norm_w"], p["norm_b"], residual=residual, save=save)
+    mark("norm")
+    qkv = torch.nn.functional.linear(f.out, p["w_qkv"]).unflatten(1, (hq + 2 * hkv, -1))
+    mark("projections (library)")
+    q, k, v = binding.varlen_attn_rotary_fwd(qkv[:, :hq], qkv[:, hq:hq + hkv], *turn, v=qkv[:, hq + hkv:])
+    mark("rotary")
+    o, lse = binding.varlen_attn_fwd(q, k, v, cu, causal, scale, max_seqlen=max_seqlen)
+    mark("attention")
+    kept = binding.varlen_attn_act8_pack([q, k, v, o], save) if save else [q, k, v, o]
+    mark("8-bit checkpoint")
+    y = torch.nn.functional.linear(o.flatten(1), p["w_out"])
+    mark("projections (library)")
+    return f.summed, y, (f.saved if save else f.summed, f.mean, f.rstd, kept, lse)
+
+
+def block_backward(torch, binding, p, dsummed, dy, saved, cu, turn, causal, scale, max_seqlen, mark=lambda name: None):
+    """Gradients of (x and residual, norm's weight and bias, w_qkv, w_out) from those of the stream and of what was added to it.  The
+    norm's output is not kept: it is formed again, from its input."""
+    hq, hkv = p["heads"]
+    h, mean, rstd, kept, lse = saved
+    packed = isinstance(kept[0], binding.Act8)
+    o, h_bf16 = binding.varlen_attn_act8_unpack([kept[3], h]) if packed else (kept[3], h)
+    mark("8-bit checkpoint")
+    dw_out = dy.T @ o.flatten(1)
+    dout = (dy @ p["w_out"]).unflatten(1, (hq, -1))
+    mark("projections (library)")
+    bwd = binding.varlen_attn_bwd_act8 if packed else binding.varlen_attn_bwd
+    dq, dk, dv = bwd(dout, *kept, lse, cu, causal, scale, max_seqlen=max_seqlen)
+    mark("attention")
+    dqkv = torch.empty((dq.shape[0], hq + 2 * hkv, dq.shape[2]), dtype=dq.dtype, device=dq.device)
+    binding.varlen_attn_rotary_bwd(dq, dk, *turn, dv=dv, dq_out=dqkv[:, :hq], dk_out=dqkv[:, hq:hq + hkv], dv_out=dqkv[:, hq + hkv:])
+    mark("rotary")
+    normed = binding.varlen_attn_norm_fwd(h_bf16, p["norm_w"], p["norm_b"]).out
+    mark("norm")
+    dw_qkv = dqkv.flatten(1).T @ normed
+    dn = dqkv.flatten(1) @ p["w_qkv"]
+    mark("projections (library)")
+    dx, dnorm_w, dnorm_b = binding.varlen_attn_norm_bwd(dn, h, mean, rstd, p["norm_w"], dsummed=dsummed)
+    mark("norm")
+    return dx, dnorm_w, dnorm_b, dw_qkv, dw_out
+
+
+def block(args, torch, binding, W):
+    """The attention half of a block, forward and backward: where the time goes, and what lies in memory between the passes."""
+    print("| batch | kept as | MB kept | step ms | norm | projections (library) | rotary | attention | 8-bit checkpoint |")
+    print("|---|---|---|---|---|---|---|---|---|", flush=True)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1234)
+    for cfg in (2, 3, 4):
+        w = W.make(cfg, lengths_only=True)
+        T, hq, hkv, d = w.total_tokens, w.num_q_heads, w.num_kv_heads, w.head_dim
+        C = hq * d
+        normal = lambda *s: torch.randn(s, device="cuda", dtype=torch.bfloat16, generator=gen)
+        p = {"heads": (hq, hkv), "norm_w": 1 + 0.1 * normal(C), "norm_b": 0.1 * normal(C),
+             "w_qkv": normal((hq + 2 * hkv) * d, C) * C ** -0.5, "w_out": normal(C, C) * C ** -0.5}
+        x, r, ds, dy = (normal(T, C) for _ in range(4))
+        cu, turn = block_positions(torch, binding, w)
+        call = (cu, turn, w.causal, w.scale, int(w.lengths.max()))
+        for save in (None, "int8", "e4m3"):
+            marks = []
+
+            def mark(name):
+                e = torch.cuda.Event(enable_timing=True)
+                e.record()
+                marks.append((name, e))
+
+            def step():
+                mark("start")
+                _, _, saved = block_forward(torch, binding, p, x, r, *call, save, mark)
+                block_backward(torch, binding, p, ds, dy, saved, *call, mark)
+                return saved
+            h, mean, rstd, kept, lse = step()
+            parts = [t for a in (h, mean, rstd, lse, *kept) for t in (a if isinstance(a, tuple) else (a,))]
+            mb = sum(t.numel() * t.element_size() for t in parts) / 1e6
+            del h, mean, rstd, kept, lse, parts
+            n = max(3, args.steps // 2)
+            marks.clear()
+            for _ in range(n):
+                step()
+            torch.cuda.synchronize()
+            names = ("norm", "projections (library)", "rotary", "attention", "8-bit checkpoint")
+            ms = {m: sum(a[1].elapsed_time(b[1]) for a, b in zip(marks, marks[1:]) if b[0] == m) / n for m in names}
+            print(f"| {w.name} ({T} tokens, {hq}/{hkv} heads of {d}) | {save or 'bf16'} | {mb:.0f} | {sum(ms.values()):.2f} | " +
+                  " | ".join(f"{ms[m]:.2f}" for m in names) + " |", flush=True)
+        del x, r, ds, dy, p
+        torch.cuda.empty_cache()
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -507,6 +618,10 @@ def main():
     ap.add_argument("--short-regime", action="store_true",
                     help="equal-length samples of 64..2048 tokens: HBM GB/s at the minimum bytes and useful "
                          "TFLOP/s, forward and backward; prints a markdown table")
+    ap.add_argument("--block", action="store_true",
+                    help="instead of the one JSON line: the attention half of a block (norm, projections, rotary, attention, "
+                         "checkpoint), forward and backward, on configs 2, 3 and 4, its input and q, k, v, o kept in bf16, "
+                         "int8 and e4m3; prints where the time goes and what is kept as a markdown table")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--headline-only", action="store_true",
                     help="leave the per-config list (configs 2, 3, 4) out of the JSON line")
@@ -550,6 +665,9 @@ def main():
         return
     if args.short_regime:
         short_regime(args, torch, binding)
+        return
+    if args.block:
+        block(args, torch, binding, W)
         return
 
     if args.calibrate_copy:
