@@ -51,14 +51,17 @@ extern "C" {
 
 enum {
     VA_OK = 0,
-    VA_ERR_NULL_PTR = 1,            /* a required pointer is NULL */
-    VA_ERR_BAD_SHAPE = 2,           /* negative size or count, heads < 1, Hq % Hkv != 0, causal not 0/1,
+    VA_ERR_NULL_PTR = 1,            /* a required pointer is NULL, or one is given without the one that goes with it */
+    VA_ERR_BAD_SHAPE = 2,           /* negative size or count, heads < 1, Hq % Hkv != 0, causal not 0/1, a stride below a
+                                       token's width, an unknown format or type,
                                        max_seqlen < 0, kv_splits or num_parts out of range */
-    VA_ERR_UNSUPPORTED = 3,         /* head_dim not in {64, 80, 96, 128}, or device is not gfx950 */
+    VA_ERR_UNSUPPORTED = 3,         /* head_dim not in {64, 80, 96, 128} (rotary positions: 2..512), more than 16384
+                                       channels, or device is not gfx950 */
     VA_ERR_WORKSPACE_TOO_SMALL = 4, /* workspace_bytes below the *_workspace_bytes() answer */
-    VA_ERR_BAD_SCALE = 5,           /* softmax_scale is NaN, infinite or negative */
+    VA_ERR_BAD_SCALE = 5,           /* softmax_scale (layer norm: eps) is NaN, infinite or negative */
     VA_ERR_HIP = 6,                 /* a HIP call failed; see varlen_attn_last_hip_error() */
-    VA_ERR_MISALIGNED = 7,          /* a tensor or workspace pointer is not 16-byte aligned */
+    VA_ERR_MISALIGNED = 7,          /* a tensor or workspace pointer is not 16-byte aligned (outside attention: not aligned
+                                       to its elements) */
     VA_ERR_BAD_CU_SEQLENS = 8,      /* varlen_attn_check_cu_seqlens only: the device array breaks the precondition */
     VA_ERR_SCRATCH_LIMIT = 9        /* varlen_attn_fwd_static_scratch only: the call needs more scratch than
                                        VA_STATIC_SCRATCH_BYTES */

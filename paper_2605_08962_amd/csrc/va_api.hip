@@ -791,13 +791,13 @@ int varlen_attn_norm_bwd(const varlen_attn_norm_params* p, const void* dy, const
 const char* varlen_attn_status_string(int status) {
     switch (status) {
         case VA_OK: return "ok";
-        case VA_ERR_NULL_PTR: return "a required pointer is NULL";
-        case VA_ERR_BAD_SHAPE: return "bad shape: negative size or count, head counts, causal flag, kv_splits, or launch too large";
-        case VA_ERR_UNSUPPORTED: return "unsupported: head_dim must be 64, 80, 96 or 128 and the device gfx950";
+        case VA_ERR_NULL_PTR: return "a required pointer is NULL, or one is given without the one that goes with it";
+        case VA_ERR_BAD_SHAPE: return "bad shape: negative size or count, head counts, causal flag, kv_splits, a stride below a token's width, an unknown format or type, or launch too large";
+        case VA_ERR_UNSUPPORTED: return "unsupported: head_dim must be 64, 80, 96 or 128 (rotary positions: 2 to 512), rows at most 16384 channels, and the device gfx950";
         case VA_ERR_WORKSPACE_TOO_SMALL: return "workspace too small";
-        case VA_ERR_BAD_SCALE: return "softmax_scale must be finite and >= 0";
+        case VA_ERR_BAD_SCALE: return "softmax_scale (layer norm: eps) must be finite and >= 0";
         case VA_ERR_HIP: return "a HIP call failed";
-        case VA_ERR_MISALIGNED: return "a tensor or workspace pointer is not 16-byte aligned";
+        case VA_ERR_MISALIGNED: return "a tensor or workspace pointer is not 16-byte aligned (outside attention: not aligned to its elements)";
         case VA_ERR_BAD_CU_SEQLENS: return "cu_seqlens must start at 0, never decrease and end at total_tokens";
         case VA_ERR_SCRATCH_LIMIT: return "the call needs more scratch than the library's static array holds (VA_STATIC_SCRATCH_BYTES)";
         default: return "unknown status";

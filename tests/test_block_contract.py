@@ -229,3 +229,56 @@ def test_tensors_beyond_two_to_the_31_elements():
     for s in rows:
         g = binding.varlen_attn_norm_fwd(q[s], wq)
         assert torch.equal(f.out[s], g.out) and torch.equal(dx[s], binding.varlen_attn_norm_bwd(q[s], q[s], g.mean, g.rstd, wq)[0])
+
+
+# What exceeds the last-level cache takes another form of the kernels: the same bits as a few of its rows by themselves.
+@pytest.mark.parametrize("h,C,fmt", [(0, 64, "e4m3"), (0, 128, None), (0, 256, "int8"), (0, 512, "e4m3"), (0, 1024, "int8"), (0, 1280, "int8"),
+                                     (0, 2048, "e4m3"), (0, 4096, "int8"), (0, 8192, None), (0, 16384, "int8"), (5, 64, None), (3, 320, "e4m3")])
+def test_large_norms_give_the_bits_of_small_ones(h, C, fmt):
+    from paper_2605_08962_amd import binding
+    T = (1 << 27) // (C * max(h, 1)) + 3
+    gen = torch.Generator(device="cuda").manual_seed(C)
+    shape = (T, h, C) if h else (T, C)
+    x, r, dy, ds = (torch.randn(shape, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(4))
+    w, b = torch.rand(C, generator=gen, device="cuda"), torch.rand(C, generator=gen, device="cuda")
+
+    def both(s):
+        f = binding.varlen_attn_norm_fwd(x[s], w, b, residual=r[s], save=fmt)
+        return [f.out, f.mean, f.rstd, f.summed, *(f.saved or ())], binding.varlen_attn_norm_bwd(dy[s], f.saved or f.summed, f.mean, f.rstd, w,
+                                                                                                  dsummed=ds[s])
+    whole, grads = both(slice(None))
+    for s in (slice(0, 40), slice(T // 2, T // 2 + 40), slice(T - 40, T)):
+        part, g = both(s)
+        _same([t[s] for t in whole] + [grads[0][s]], part + [g[0]])
+    mean, rstd = whole[1].double()[..., None], whole[2].double()[..., None]
+    seen = B.act8_values(*whole[4:]) if fmt else whole[3]
+    dw = (dy.double() * ((seen.double() - mean) * rstd))
+    # a thread adds up at most T h / 512 rows (64 channels: 2^21 / 32768), then 32 row groups and 32 + 32 partial sums: under 400 additions
+    B.assert_within("dw", grads[1], dw.flatten(0, -2).sum(0), 400 * B.U32 * dw.abs().flatten(0, -2).sum(0))
+    B.assert_within("db", grads[2], dy.double().flatten(0, -2).sum(0), 400 * B.U32 * dy.double().abs().flatten(0, -2).sum(0))
+
+
+@pytest.mark.parametrize("hq,hkv,d,P,interleaved", [(16, 16, 64, 32, False), (8, 2, 128, 64, False), (8, 8, 80, 40, False), (8, 4, 96, 48, True),
+                                                    (8, 4, 128, 32, False), (4, 4, 80, 18, True), (3, 3, 66, 33, False)])
+def test_large_rotations_and_packings_give_the_bits_of_small_ones(hq, hkv, d, P, interleaved):
+    from paper_2605_08962_amd import binding
+    T = (1 << 27) // ((hq + 2 * hkv) * d) + 5
+    gen = torch.Generator(device="cuda").manual_seed(d)
+    qkv = torch.randn((T, hq + 2 * hkv, d), generator=gen, device="cuda").to(torch.bfloat16)
+    pos = torch.randint(0, 1 << 20, (2, T), generator=gen, device="cuda", dtype=torch.int32)
+    freq, axis = torch.rand(P, generator=gen, device="cuda"), (torch.arange(P, device="cuda") % 2).int()
+
+    def turn(x, pos, **kw):
+        return binding.varlen_attn_rotary_fwd(x[:, :hq], x[:, hq:hq + hkv], pos, freq, axis, v=x[:, hq + hkv:], interleaved=interleaved, **kw)
+    whole = turn(qkv, pos)
+    packed = binding.varlen_attn_act8_pack(list(whole), "e4m3")
+    back = binding.varlen_attn_act8_unpack(packed)
+    for s in (slice(0, 40), slice(T // 2, T // 2 + 40), slice(T - 40, T)):
+        part = turn(qkv[s], pos[:, s].contiguous())
+        _same([t[s] for t in whole], list(part))
+        p = binding.varlen_attn_act8_pack(list(part), "e4m3")
+        _same([t[s] for x in packed for t in x], [t for x in p for t in x])
+        _same([t[s] for t in back], binding.varlen_attn_act8_unpack(p))
+    views = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    turn(qkv, pos, q_out=views[0], k_out=views[1], v_out=views[2])  # in place
+    _same(list(whole), list(views))
