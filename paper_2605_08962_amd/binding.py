@@ -685,6 +685,12 @@ def _check_weights(weight, bias, channels):
     return 0 if weight is None else _WEIGHT_TYPES[weight.dtype]
 
 
+def _statistics_like(t, shape, name):
+    if t is not None:
+        _require(t, torch.float32, name)
+        _out_like(t, shape[:-1], name)
+
+
 def _contiguous_like(t, shape, name):
     if t is not None:
         _require(t, torch.bfloat16, name)
@@ -696,16 +702,17 @@ def _norm_params(shape, weight_type, act8_format, eps, x_stride=0, dy_stride=0, 
                       dx_stride)
 
 
-def varlen_attn_norm_fwd(x, weight=None, bias=None, eps=1e-5, residual=None, save=None, out=None, stream=None):
+def varlen_attn_norm_fwd(x, weight=None, bias=None, eps=1e-5, residual=None, save=None, out=None, mean=None, rstd=None, summed=None,
+                         saved=None, stream=None):
     """Layer norm over the last dimension of x, bf16 [T, C] or [T, H, C] (contiguous or a part of a wider tensor): a NormForward
     (out bf16, mean and rstd fp32 [T] or [T, H], summed, saved); asynchronous on the stream.
     weight, bias: bf16 or fp32 [C], or None.  residual: contiguous, x's shape; the norm is then of summed = bf16(x + residual).
     save: "int8" or "e4m3": what is normed is left in 8 bits too (saved, an Act8), for varlen_attn_norm_bwd.
-    out: the caller's own contiguous tensor of x's shape."""
+    out, mean, rstd, summed (with residual), saved (with save, an Act8): the caller's own, contiguous, of those shapes."""
     if save is not None and save not in _ACT8_FORMATS:
         raise ValueError("save must be int8 or e4m3")
     number, code_type = _ACT8_FORMATS[save or "int8"]
-    if stream is None:
+    if stream is None and mean is None and rstd is None and summed is None and saved is None:
         answer = (_host or _load_host()).norm_fwd(x, weight, bias, float(eps), residual, number if save else None, out)
         if _done(answer):
             return NormForward._make(answer)
@@ -713,12 +720,23 @@ def varlen_attn_norm_fwd(x, weight=None, bias=None, eps=1e-5, residual=None, sav
     shape = x.shape
     _contiguous_like(residual, shape, "residual")
     _contiguous_like(out, shape, "out")
+    _contiguous_like(summed, shape, "summed")
+    _statistics_like(mean, shape, "mean")
+    _statistics_like(rstd, shape, "rstd")
+    if summed is not None and residual is None:
+        raise ValueError("residual must be given with summed")
+    if saved is not None and (save is None or _check_act8(saved, "saved") != number or saved.codes.shape != shape):
+        raise ValueError("saved must match x and save")
     p = _norm_params(shape, _check_weights(weight, bias, shape[-1]), number, eps, x_stride=stride)
-    with _On(x, stream, weight=weight, bias=bias, residual=residual, out=out) as on:
+    with _On(x, stream, weight=weight, bias=bias, residual=residual, out=out, mean=mean, rstd=rstd, summed=summed,
+             saved=None if saved is None else saved.codes) as on:
         out = on.empty(shape, torch.bfloat16) if out is None else out
-        mean, rstd = on.empty(shape[:-1], torch.float32), on.empty(shape[:-1], torch.float32)
-        summed = None if residual is None else on.empty(shape, torch.bfloat16)
-        saved = None if save is None else Act8(on.empty(shape, code_type), on.empty(_act8_shape(shape), torch.float32))
+        mean = on.empty(shape[:-1], torch.float32) if mean is None else mean
+        rstd = on.empty(shape[:-1], torch.float32) if rstd is None else rstd
+        if residual is not None and summed is None:
+            summed = on.empty(shape, torch.bfloat16)
+        if save is not None and saved is None:
+            saved = Act8(on.empty(shape, code_type), on.empty(_act8_shape(shape), torch.float32))
         codes, scales = saved or (None, None)
         _check(load().varlen_attn_norm_fwd(ctypes.byref(p), x.data_ptr(), _ptr(residual), _ptr(weight), _ptr(bias), out.data_ptr(),
                                            _ptr(summed), mean.data_ptr(), rstd.data_ptr(), _ptr(codes), _ptr(scales), on.stream))
@@ -729,12 +747,12 @@ def norm_bwd_workspace_bytes(params):
     return int(load().varlen_attn_norm_bwd_workspace_bytes(ctypes.byref(params)))
 
 
-def varlen_attn_norm_bwd(dy, x, mean, rstd, weight=None, dsummed=None, dx=None, workspace=None, stream=None):
+def varlen_attn_norm_bwd(dy, x, mean, rstd, weight=None, dsummed=None, dx=None, dweight=None, dbias=None, workspace=None, stream=None):
     """(dx bf16, dweight fp32, dbias fp32; the last two None without weight) of varlen_attn_norm_fwd; asynchronous on the stream.
     x: what was normed: the forward's x, its summed where it had a residual, or its saved Act8.  mean, rstd: the forward's.
     dsummed: the gradient that reaches summed on its own way, added to dx (which is the gradient of x and of residual).
-    dy, x and dx may be parts of wider tensors; dx, workspace: the caller's own."""
-    if stream is None and workspace is None:
+    dy, x and dx may be parts of wider tensors; dx, dweight and dbias (with weight), workspace: the caller's own."""
+    if stream is None and dweight is None and dbias is None and workspace is None:
         answer = (_host or _load_host()).norm_bwd(dy, x, mean, rstd, weight, dsummed, dx)
         if _done(answer):
             return answer
@@ -747,6 +765,12 @@ def varlen_attn_norm_bwd(dy, x, mean, rstd, weight=None, dsummed=None, dx=None, 
     for t, n in ((mean, "mean"), (rstd, "rstd")):
         _require(t, torch.float32, n)
         _out_like(t, shape[:-1], n)
+    for t, n in ((dweight, "dweight"), (dbias, "dbias")):
+        if t is not None and weight is None:
+            raise ValueError(f"weight must be given with {n}")
+        if t is not None:
+            _require(t, torch.float32, n)
+            _out_like(t, shape[-1:], n)
     _contiguous_like(dsummed, shape, "dsummed")
     dx_stride = shape[1:].numel()
     if dx is not None:
@@ -755,11 +779,12 @@ def varlen_attn_norm_bwd(dy, x, mean, rstd, weight=None, dsummed=None, dx=None, 
     _require_room(workspace, None, "workspace")
     p = _norm_params(shape, _check_weights(weight, None, shape[-1]), number, 0.0, x_stride, dy_stride, dx_stride)
     codes, scales = x if packed else (None, None)
-    with _On(dy, stream, x=x.codes if packed else x, mean=mean, rstd=rstd, weight=weight, dsummed=dsummed, dx=dx) as on:
+    with _On(dy, stream, x=x.codes if packed else x, mean=mean, rstd=rstd, weight=weight, dsummed=dsummed, dx=dx, dweight=dweight,
+             dbias=dbias) as on:
         dx = on.empty(shape, torch.bfloat16) if dx is None else dx
-        dweight = dbias = None
         if weight is not None:
-            dweight, dbias = on.empty(shape[-1:], torch.float32), on.empty(shape[-1:], torch.float32)
+            dweight = on.empty(shape[-1:], torch.float32) if dweight is None else dweight
+            dbias = on.empty(shape[-1:], torch.float32) if dbias is None else dbias
             if workspace is None:
                 workspace = on.scratch(norm_bwd_workspace_bytes(p))
         _check(load().varlen_attn_norm_bwd(ctypes.byref(p), dy.data_ptr(), None if packed else x.data_ptr(), _ptr(codes), _ptr(scales),

@@ -197,16 +197,17 @@ def _a8(*shape, code=torch.int8):
 
 
 def _fwd_call(**o):
-    a = dict(x=bf(T, 96), weight=bf(96), bias=bf(96), residual=bf(T, 96), save=None, out=None)
+    a = dict(x=bf(T, 96), weight=bf(96), bias=bf(96), residual=bf(T, 96), save=None, out=None, mean=None, summed=None, saved=None)
     a.update(o)
-    return lambda b: b.varlen_attn_norm_fwd(a["x"], a["weight"], a["bias"], residual=a["residual"], save=a["save"], out=a["out"])
+    return lambda b: b.varlen_attn_norm_fwd(a["x"], a["weight"], a["bias"], residual=a["residual"], save=a["save"], out=a["out"],
+                                            mean=a["mean"], summed=a["summed"], saved=a["saved"])
 
 
 def _bwd_call(**o):
-    a = dict(dy=bf(T, 96), x=bf(T, 96), mean=torch.zeros(T), rstd=torch.zeros(T), weight=bf(96), dsummed=None, dx=None, ws=None)
+    a = dict(dy=bf(T, 96), x=bf(T, 96), mean=torch.zeros(T), rstd=torch.zeros(T), weight=bf(96), dsummed=None, dx=None, dw=None, ws=None)
     a.update(o)
     return lambda b: b.varlen_attn_norm_bwd(a["dy"], a["x"], a["mean"], a["rstd"], a["weight"], dsummed=a["dsummed"], dx=a["dx"],
-                                            workspace=a["ws"])
+                                            dweight=a["dw"], workspace=a["ws"])
 
 
 def _attn_call(**o):
@@ -245,6 +246,10 @@ BAD = [
     (_fwd_call, dict(bias=torch.zeros(96)), "bias must have"), (_fwd_call, dict(residual=bf(T, 95)), "residual must"),
     (_fwd_call, dict(residual=bf(T, 192)[:, ::2]), "residual must"), (_fwd_call, dict(save="e5m2"), "save must"),
     (_fwd_call, dict(out=bf(T, 192)[:, :96]), "out must"), (_fwd_call, dict(out=bf(T + 1, 96)), "out must"),
+    (_fwd_call, dict(mean=torch.zeros(T, 1)), "mean must"), (_fwd_call, dict(summed=bf(T, 97)), "summed must"),
+    (_fwd_call, dict(residual=None, summed=bf(T, 96)), "residual must be given"), (_fwd_call, dict(saved=_a8(T, 96)), "saved must match"),
+    (_fwd_call, dict(save="e4m3", saved=_a8(T, 96)), "saved must match"), (_bwd_call, dict(dw=torch.zeros(95)), "dweight must"),
+    (_bwd_call, dict(dw=torch.zeros(96), weight=None), "weight must be given"),
     (_bwd_call, dict(x=bf(T, 95)), "x must match"), (_bwd_call, dict(x=_a8(T, 95)), "x must match"), (_bwd_call, dict(mean=torch.zeros(T + 1)), "mean must"),
     (_bwd_call, dict(rstd=torch.zeros(T).double()), "rstd must"), (_bwd_call, dict(dsummed=bf(T - 1, 96)), "dsummed must"),
     (_bwd_call, dict(dx=bf(T, 97)), "dx must"), (_bwd_call, dict(dx=bf(1, 96).expand(T, -1)), "dx must hold"),
@@ -259,6 +264,7 @@ GOOD = [
     (_rotary_call, {}), (_rotary_call, dict(v=None)), (_rotary_call, dict(q=bf(T, HQ + 2 * HKV, D)[:, 1:5])), (_rotary_call, dict(q_out=bf(T, 9, D)[:, :HQ])),
     (_rotary_call, dict(q=bf(2 * T, HQ, D)[::2])), (_pos_call, {}), (_pos_call, dict(first=None)), (_fwd_call, {}), (_fwd_call, dict(save="e4m3", bias=None)),
     (_fwd_call, dict(x=bf(T, 3, 96)[:, 1:], residual=bf(T, 2, 96), weight=torch.zeros(96), bias=torch.zeros(96))), (_bwd_call, {}),
+    (_fwd_call, dict(save="int8", saved=_a8(T, 96), mean=torch.zeros(T), summed=bf(T, 96))), (_bwd_call, dict(dw=torch.zeros(96))),
     (_bwd_call, dict(x=_a8(T, 96), weight=None)), (_attn_call, {}), (_attn_call, dict(ws=torch.zeros(1 << 20, dtype=torch.uint8), dq=bf(T * HQ * D))),
 ]
 

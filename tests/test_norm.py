@@ -163,3 +163,21 @@ def test_the_same_call_gives_the_same_bits():
     first = binding.varlen_attn_norm_bwd(dy, x, f.mean, f.rstd, w)
     for _ in range(3):
         assert all(torch.equal(a, c) for a, c in zip(binding.varlen_attn_norm_bwd(dy, x, f.mean, f.rstd, w), first))
+
+
+def test_results_go_where_the_caller_says():
+    from paper_2605_08962_amd import binding
+    x, w, b, dy = _inputs((70, 200), torch.float32, seed=9)
+    f = binding.varlen_attn_norm_fwd(x, w, b, residual=dy, save="int8")
+    mine = binding.NormForward(*(binding.Act8(*map(torch.zeros_like, t)) if isinstance(t, tuple) else torch.zeros_like(t) for t in f))
+    got = binding.varlen_attn_norm_fwd(x, w, b, residual=dy, save="int8", **mine._asdict())
+    assert all(a is m for a, m in zip(got, mine))
+    for a, m in zip((*f[:4], *f.saved), (*mine[:4], *mine.saved)):
+        assert torch.equal(a, m)
+    want = binding.varlen_attn_norm_bwd(dy, f.saved, f.mean, f.rstd, w)
+    outs = [torch.zeros_like(t) for t in want]
+    ws = torch.empty(binding.norm_bwd_workspace_bytes(binding.NormParams(70, 1, 200, 1, 0, 0.0, 200, 200, 200)), dtype=torch.uint8, device="cuda")
+    got = binding.varlen_attn_norm_bwd(dy, f.saved, f.mean, f.rstd, w, dx=outs[0], dweight=outs[1], dbias=outs[2], workspace=ws)
+    assert all(a is m and torch.equal(a, t) for a, m, t in zip(got, outs, want))
+    with pytest.raises(binding.VarlenAttnError, match="workspace too small"):
+        binding.varlen_attn_norm_bwd(dy, f.saved, f.mean, f.rstd, w, workspace=ws[:-256])
