@@ -212,15 +212,16 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
     for (int64_t base = (int64_t)blockIdx.x * R::ROWS; base < a.rows; base += step, row += step) {
         const bool there = row < a.rows;
         Row now = next;
-        // d = h - mean, dy and g = dy w of run j.  Formed twice, for the sums and for dx: kept, they would be 24 registers a run
-        // instead of 8 or 6, which is a wave per SIMD or two.  Behind the row's end dy, and so g, is zero.
-        auto run = [&](int j, float* d, float* dy, float* g) {
+        // n = (h - mean) rstd, dy and g = dy w of run j; `plain`: h - mean in place of n, where the row is in bf16.  Formed twice, for
+        // the sums and for dx: kept, they would be 24 registers a run instead of 8 or 6, which is a wave per SIMD or two.  In 8 bits n
+        // is one product and sum from the code.  Behind the row's end dy, and so g, is zero.
+        auto run = [&](int j, bool plain, float* n, float* dy, float* g) {
             if constexpr (FORMAT < 0) {
-                to_float8(now.x[j], d);
+                to_float8(now.x[j], n);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] -= now.mean;
+                for (int e = 0; e < 8; ++e) n[e] = plain ? n[e] - now.mean : (n[e] - now.mean) * now.rstd;
             } else {
-                act8_decode(now.codes[j], now.scale[j], FORMAT, d, now.mean);
+                act8_decode(now.codes[j], now.scale[j] * now.rstd, FORMAT, n, now.mean * now.rstd);
             }
             to_float8(now.dy[j], dy);
             u.weight.get(j, lane, g);
@@ -239,19 +240,19 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            float d[8], dy[8], g[8];
-            run(j, d, dy, g);
+            float n[8], dy[8], g[8];
+            run(j, false, n, dy, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                dw[j][e] += dy[e] * now.rstd * d[e];
+                dw[j][e] += dy[e] * n[e];
                 db[j][e] += dy[e];
                 sum[0] += g[e];
-                sum[1] += g[e] * d[e];
+                sum[1] += g[e] * n[e];
             }
         }
         row_sum<G>(sum, lds, at);
-        // dx = rstd (g - sum g / C - n sum(g n) / C) with n = d rstd
-        const float c0 = -now.rstd * (sum[0] / (float)C), c1 = -now.rstd * (now.rstd * (now.rstd * sum[1] / (float)C));
+        // dx = rstd (g - sum g / C - n sum(g n) / C)
+        const float c0 = -now.rstd * (sum[0] / (float)C), cn = -now.rstd * (sum[1] / (float)C), c1 = FORMAT < 0 ? cn * now.rstd : cn;
         uint16_t* const out = (uint16_t*)a.dx + row_offset(a, row, a.dx_stride);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {  // (the compiler must not see that it has formed them before)
@@ -262,10 +263,10 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = 8 * (lane + j * G), left = there ? C - col : 0;
-            float dx[8], d[8], dy[8], g[8];
-            run(j, d, dy, g);
+            float dx[8], n[8], dy[8], g[8];
+            run(j, true, n, dy, g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dx[e] = g[e] * now.rstd + (d[e] * c1 + c0);
+            for (int e = 0; e < 8; ++e) dx[e] = g[e] * now.rstd + (n[e] * c1 + c0);
             if (a.dsummed) {
                 float r[8];
                 to_float8(ds[j], r);
