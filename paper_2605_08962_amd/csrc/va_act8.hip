@@ -1,5 +1,5 @@
 // Checkpoints of activations in 8 bits (the format: va_ops.h): several tensors packed or unpacked by one launch.
-// Bound by memory: 3 bytes and a few operations per channel.
+// Bound by memory: 3 bytes and some 5 operations per channel.
 #include "va_internal.h"
 #include "va_ops.h"
 

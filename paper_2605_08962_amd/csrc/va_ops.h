@@ -41,6 +41,17 @@ __device__ __forceinline__ float lanes_sum(float x) {
         return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
     }));
 }
+// Sum of x over the wave's groups of G lanes, lane i of each: every group ends with the same bits.
+template <int G>
+__device__ __forceinline__ float groups_sum(float x) {
+    if (G <= 8) x += __uint_as_float(dpp<0x128>(__float_as_uint(x)));  // rotated by 8 within 16 lanes
+    if (G <= 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (G <= 32) x = xhalf_sum(x);
+    return x;
+}
 template <int G>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
     return lanes_reduce<G>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });

@@ -4,7 +4,8 @@
 //     phi = positions[pair_axis[j]][t] * inv_freq[j]:    y1 = x1 cos phi - x2 sin phi,   y2 = x2 cos phi + x1 sin phi;
 // the backward pass turns by -phi (the inverse of a rotation is its transpose).  Channels from 2P on, and all of v, are copied.
 // Bound by memory: 4 bytes per channel moved against 3 operations; the angles are formed once per token and pair and shared by
-// its heads through LDS.
+// its heads through LDS.  178572 tokens, 16/16 heads of 64, out of the fused projection 375 us (5.9 TB/s), 32768 tokens, 32/8 heads of 128
+// 134 us (6.0 TB/s).
 #include "va_internal.h"
 #include "va_ops.h"
 
@@ -170,8 +171,8 @@ __device__ __forceinline__ u32x4 from_lane_xor(const u32x4& w, bool upper) {
 // it is written.  Where a run's pairs' other channels are:
 //   HERE      in the run itself (interleaved)        LANE4, LANE8   4 or 8 lanes on (whole heads of 64 and 128 channels)
 //   MEMORY    elsewhere: read once more, out of the line that another thread of the tile has just fetched
-// STREAMED: past the caches.  Measured, TB/s forward, one / two / three / four runs a thread, through the caches and past them (and all
-// loads of the pair, halves written by one thread: 5.25, 5.2, 4.9, 4.8 at best)
+// STREAMED: past the caches.  Measured, TB/s forward, one / two / three / four runs a thread, through the caches / past them (where one
+// thread took both halves of a pair instead: 5.46, 5.33, 5.04 and, interleaved, 4.96 at best)
 //   178572 x 16/16 heads of 64   5.80 5.90 5.68 5.53 / 5.46 6.05 6.03 6.01       32768 x 32/8 of 128   5.54 5.60 5.55 5.53 / 5.56 5.89 6.02 6.12
 //   100000 x 16/16 of 80         4.55 5.40 5.41 4.99 / 4.58 5.03 5.82 5.10       ... interleaved       5.71 5.56 5.54 5.39 / 5.48 6.00 6.09 5.96
 enum RotaryPartner { HERE, LANE4, LANE8, MEMORY };
@@ -267,7 +268,8 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_flat_kernel(RotaryArgs a) 
 // Position of every packed token.  Segment s holds the rows [cu[s], cu[s + 1]); grids[s] = (time, height, width) of an image or
 // video, whose patches lie time by time in blocks of merge x merge, rows of blocks one after the other; a height or width below 1
 // means text, which advances on all three axes.  first[s] is added to all.  Tokens outside every segment get 0.
-// One thread a token finds its segment by bisection; no contents of cu or grids lead outside the tensors.
+// One thread a token finds its segment by bisection; no contents of cu or grids lead outside the tensors.  Bound by latency, a dozen
+// loads one after the other: 609226 tokens in 400 segments 6.5 us, 246 in 4 1.9 us.
 __global__ void __launch_bounds__(256)
 positions_kernel(int total_tokens, int num_segments, int merge, const int32_t* __restrict__ cu, const int32_t* __restrict__ grids,
                  const int32_t* __restrict__ first, int32_t* __restrict__ positions) {
