@@ -5,7 +5,7 @@
 // off zero loses nothing.  The forward can leave h in 8 bits (va_ops.h) in the same pass, for the backward to read.
 // Bound by memory: 4 to 9 bytes per channel against some 10 operations forward and 15 backward.  What the counters read and write is
 // what the formulas need.  Forward / backward: 178572 x 1024 with residual 251 / 261 us (5.8 / 5.6 TB/s), 65537 x 1280 with and from
-// int8 72 / 83 us (5.8 / 5.1: half of the vector unit's issue slots), 32768 x 32 heads of 128 93 / 148 us (5.7 / 5.4).
+// int8 72 / 82 us (5.8 / 5.2: half of the vector unit's issue slots), 32768 x 32 heads of 128 92 / 144 us (5.8 / 5.6).
 //
 // G threads hold a row, NV runs of 8 channels each: run j of thread i are the channels 8 (i + j G)...  Threads of a workgroup
 // beyond that take further rows.  A workgroup walks rows with the stride of the grid, so that weight and bias are brought into LDS
@@ -48,6 +48,20 @@ __device__ __forceinline__ void row_sum(float (&x)[N], float (*lds)[4][RowGroup<
         }
         at ^= 1;
     }
+}
+
+// s / C and v^-1/2 without the library's care for the ends of the range, which is 45 instructions a row beside the 130 of a thread with 8
+// channels of it (32768 x 32 heads of 80, forward / backward, 75.5 / 111.5 -> 73.2 / 103.2 us).  The quotient is corrected by its
+// remainder (exact where the true one is), the root by one Newton step, to within 2^-23 of it; numbers that this is not for take the
+// long way.
+__device__ __forceinline__ float over(float s, float c, float inv_c) {
+    const float q = s * inv_c;
+    return fabsf(q) < INFINITY ? fmaf(fmaf(-q, c, s), inv_c, q) : q;
+}
+__device__ __forceinline__ float inverse_root(float v) {
+    if (!(v >= 0x1p-100f && v <= 0x1p100f)) return 1.f / sqrtf(v);
+    const float y = __builtin_amdgcn_rsqf(v), half = 0.5f * y;
+    return fmaf(half, fmaf(-v * y, y, 1.f), y);
 }
 
 // Weight or bias in fp32 in LDS, as threads of a row read them: 16 bytes a thread, neighbours side by side.  (In registers they
@@ -135,6 +149,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
     __shared__ Weights<G, NV> weight, bias;
     int at = 0;
     const int C = a.channels, lane = threadIdx.x % G;
+    const float inv_c = 1.f / (float)C;
     const int blocks = (C + kAct8Block - 1) / kAct8Block;
     const int64_t step = (int64_t)gridDim.x * R::ROWS;
     u32x4 xs[NV], rs[NV];
@@ -184,7 +199,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
         walk.advance(next);
         fetch();  // (in flight while this row is worked on)
         row_sum<G>(sum, lds, at);
-        const float mean = sum[0] / (float)C;
+        const float mean = over(sum[0], (float)C, inv_c);
         float sq[1] = {0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -199,7 +214,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_fwd_kernel(NormArgs
             sq[0] += n > 0 ? run : 0.f;
         }
         row_sum<G>(sq, lds, at);
-        const float rstd = 1.f / sqrtf(sq[0] / (float)C + a.eps);
+        const float rstd = inverse_root(over(sq[0], (float)C, inv_c) + a.eps);
         if (there && lane == 0) {
             a.mean[row] = mean;
             a.rstd[row] = rstd;
@@ -228,6 +243,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
     } u;
     int at = 0;
     const int C = a.channels, lane = threadIdx.x % G;
+    const float inv_c = 1.f / (float)C;
     const int blocks = (C + kAct8Block - 1) / kAct8Block;
     float dw[NV][8] = {}, db[NV][8] = {};
     const int64_t step = (int64_t)gridDim.x * R::ROWS;
@@ -303,7 +319,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
         }
         row_sum<G>(sum, lds, at);
         // dx = rstd (g - sum g / C - n sum(g n) / C)
-        const float c0 = -now.rstd * (sum[0] / (float)C), cn = -now.rstd * (sum[1] / (float)C), c1 = FORMAT < 0 ? cn * now.rstd : cn;
+        const float c0 = -now.rstd * (sum[0] * inv_c), cn = -now.rstd * (sum[1] * inv_c), c1 = FORMAT < 0 ? cn * now.rstd : cn;
         uint16_t* const out = (uint16_t*)a.dx + out_at;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {  // (the compiler must not see that it has formed them before)
@@ -419,10 +435,12 @@ int norm_bwd_wgs(int64_t rows, int C) {
 #undef VA_NORM_GO
 }
 
-// What is moved past the caches: more than the last one's 256 MB, which nobody finds there again.
+// What is moved past the caches: more than the last one's 256 MB, which nobody finds there again; if what a wave moves at a time, one row
+// or several short ones, is whole lines (32768 x 32 heads of 96 channels, forward / backward, 4.8 / 4.9 -> 5.05 / 5.15 TB/s).
 static int norm_mode(const NormArgs& a, int bytes_per_channel) {
-    if (a.channels % 8) return RAGGED;
-    return a.channels % 64 == 0 && a.rows * a.channels * bytes_per_channel > (int64_t)256 << 20 ? STREAM : WIDE;
+    const int C = a.channels, rows = C <= 64 ? 8 : C <= 128 ? 4 : C <= 256 ? 2 : 1;
+    if (C % 8) return RAGGED;
+    return rows * C % 64 == 0 && a.rows * C * bytes_per_channel > (int64_t)256 << 20 ? STREAM : WIDE;
 }
 
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t stream) {

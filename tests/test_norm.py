@@ -140,6 +140,7 @@ def test_rows_that_are_no_numbers_stay_by_themselves():
     bad = torch.zeros(40, dtype=torch.bool, device="cuda")
     bad[[3, 20]] = True
     assert torch.isnan(f.out[bad]).all() and torch.equal(f.out[~bad], clean.out[~bad])
+    assert torch.isnan(f.mean[3]) and torch.isposinf(f.mean[20]) and torch.isnan(f.rstd[bad]).all()
     dx = binding.varlen_attn_norm_bwd(dy, y, f.mean, f.rstd, w)[0]
     want = binding.varlen_attn_norm_bwd(dy, x, clean.mean, clean.rstd, w)[0]
     assert torch.isnan(dx[bad]).all() and torch.equal(dx[~bad], want[~bad])
@@ -181,3 +182,16 @@ def test_results_go_where_the_caller_says():
     assert all(a is m and torch.equal(a, t) for a, m, t in zip(got, outs, want))
     with pytest.raises(binding.VarlenAttnError, match="workspace too small"):
         binding.varlen_attn_norm_bwd(dy, f.saved, f.mean, f.rstd, w, workspace=ws[:-256])
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-5, 1e20])
+def test_statistics_at_the_ends_of_the_range(eps):
+    """Variances from 2^-120 to 2^110, with and without an eps beside them."""
+    from paper_2605_08962_amd import binding
+    x = B.bf(60, 192, seed=4) * (2.0 ** torch.arange(-60, 60, 2, device="cuda"))[:, None]
+    x = x.to(torch.bfloat16)
+    f = binding.varlen_attn_norm_fwd(x, eps=eps)
+    (y, y_off), (mean, mean_off), (rstd, rstd_off) = B.norm(x, None, None, float(torch.tensor(eps)))
+    B.assert_within("mean", f.mean, mean, mean_off)
+    B.assert_within("rstd", f.rstd, rstd, rstd_off)
+    B.assert_within("y", f.out, y, y_off + 1e-37)  # (a bf16 below 2^-126 has fewer bits)
