@@ -136,6 +136,25 @@ def test_positions(merge, grids, based):
         assert torch.equal(binding.varlen_attn_rotary_positions(dev(cu), dev(grids), total, first=dev(first), merge=merge), got)
 
 
+@pytest.mark.parametrize("seed,segments,longest,empty", [(1, 70, 3, 0.9), (2, 500, 2, 0.95), (3, 64, 1, 0.0), (4, 65, 1, 0.0), (5, 300, 200, 0.3),
+                                                          (6, 20000, 4, 0.5), (7, 4097, 1, 0.99), (8, 1, 700, 0.0), (9, 129, 64, 0.0)])
+def test_positions_of_short_and_empty_segments(seed, segments, longest, empty):
+    """Few and many of them to a wave of tokens, and a wave that no segment or every one ends in."""
+    from paper_2605_08962_amd import binding
+    gen = torch.Generator().manual_seed(seed)
+    lens = torch.randint(1, longest + 1, (segments,), generator=gen)
+    lens[torch.rand(segments, generator=gen) < empty] = 0
+    cu = torch.cat([torch.zeros(1, dtype=torch.long), lens.cumsum(0)])
+    first = torch.randint(0, 1000, (segments,), generator=gen)
+    total = int(cu[-1]) + 70  # (and tokens behind the last)
+    seg = torch.repeat_interleave(torch.arange(segments), lens)
+    want = torch.zeros(total, dtype=torch.int32)
+    want[:len(seg)] = (torch.arange(len(seg)) - cu[seg] + first[seg]).int()
+    dev = lambda x: x.to(torch.int32).cuda()  # noqa: E731
+    got = binding.varlen_attn_rotary_positions(dev(cu), torch.zeros((segments, 3), dtype=torch.int32, device="cuda"), total, first=dev(first))
+    assert torch.equal(got.cpu(), want.expand(3, -1))
+
+
 def test_positions_of_many_and_of_no_segments():
     from paper_2605_08962_amd import binding
     n = 5000
