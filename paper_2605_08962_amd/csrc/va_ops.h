@@ -159,15 +159,12 @@ __device__ __forceinline__ u32x2 act8_encode(const float* x, float scale, int fo
     }
     return w;
 }
-// code * scale - off (off = 0: with the one rounding that the format's value has).
+// code * scale - off (off = 0: with the one rounding that the format's value has).  The product is formed from the signed code, never
+// from code + 128: 128 * scale is beyond fp32 where a block holds one of bf16's two largest numbers.
 __device__ __forceinline__ void act8_decode(const u32x2& w, float scale, int format, float* x, float off = 0.f) {
     if (format == VA_ACT8_INT8) {
-        // code + 128 as an unsigned byte: one conversion, and 128 scale comes off again exactly, with the one rounding of the product
-        u32x2 b = w ^ 0x80808080u;
-        asm("" : "+v"(b));  // (or the compiler flips each byte by itself, an instruction a channel)
-        const float low = -128.f * scale - off;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = fmaf((float)((b[e >> 2] >> (8 * (e & 3))) & 255u), scale, low);
+        for (int e = 0; e < 8; ++e) x[e] = fmaf((float)(int8_t)(w[e >> 2] >> (8 * (e & 3))), scale, -off);
     } else {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
