@@ -318,8 +318,9 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
             }
         }
         row_sum<G>(sum, lds, at);
-        // dx = rstd (g - sum g / C - n sum(g n) / C)
-        const float c0 = -now.rstd * (sum[0] * inv_c), cn = -now.rstd * (sum[1] * inv_c), c1 = FORMAT < 0 ? cn * now.rstd : cn;
+        // dx = rstd (g - n sum(g n) / C) - rstd sum g / C.  (rstd^2, which the other order forms from h - mean, is beyond fp32 for rows of
+        // next to no variance.)
+        const float cn = -(sum[1] * inv_c), c1 = FORMAT < 0 ? now.rstd * cn : cn, c0 = -now.rstd * (sum[0] * inv_c);
         uint16_t* const out = (uint16_t*)a.dx + out_at;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {  // (the compiler must not see that it has formed them before)
@@ -333,7 +334,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
             float dx[8], n[8], dy[8], g[8];
             run(j, true, n, dy, g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dx[e] = g[e] * now.rstd + (n[e] * c1 + c0);
+            for (int e = 0; e < 8; ++e) dx[e] = (g[e] + n[e] * c1) * now.rstd + c0;
             if (a.dsummed) {
                 float r[8];
                 to_float8(ds[j], r);
