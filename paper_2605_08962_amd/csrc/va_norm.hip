@@ -280,14 +280,20 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
         Row now = next;
         // n = (h - mean) rstd, dy and g = dy w of run j; `plain`: h - mean in place of n, where the row is in bf16.  Formed twice, for
         // the sums and for dx: kept, they would be 24 registers a run instead of 8 or 6, which is a wave per SIMD or two.  In 8 bits n
-        // is one product and sum from the code.  Behind the row's end dy, and so g, is zero.
+        // is one product and sum from the code.  Behind the row's end dy, and so g, is zero, and n is no infinity (mean rstd may be one).
         auto run = [&](int j, bool plain, float* n, float* dy, float* g) {
+            const int left = C - 8 * (lane + j * G);
+            const float rstd = MODE == RAGGED || left > 0 ? now.rstd : 0.f;
             if constexpr (FORMAT < 0) {
                 to_float8(now.x[j], n);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) n[e] = plain ? n[e] - now.mean : (n[e] - now.mean) * now.rstd;
+                for (int e = 0; e < 8; ++e) n[e] = plain ? n[e] - now.mean : (n[e] - now.mean) * rstd;
             } else {
-                act8_decode(now.codes[j], now.scale[j] * now.rstd, FORMAT, n, now.mean * now.rstd);
+                act8_decode(now.codes[j], now.scale[j] * rstd, FORMAT, n, now.mean * rstd);
+            }
+            if (MODE == RAGGED && !plain && left < 8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) n[e] = e < left ? n[e] : 0.f;
             }
             to_float8(now.dy[j], dy);
             u.weight.get(j, lane, g);

@@ -30,3 +30,22 @@ def test_rows_of_next_to_no_variance(shape, weights, eps):
     if w is not None:
         B.assert_within("dw", got[1], dw, dw_off)
         B.assert_within("db", got[2], db, db_off)
+
+
+@pytest.mark.parametrize("weights", [torch.float32, None])
+@pytest.mark.parametrize("shape", [(7, 8), (7, 40), (7, 128), (7, 200), (7, 1001), (7, 1537), (7, 2056), (7, 4104), (7, 8200), (5, 3, 80), (5, 3, 30)])
+def test_constant_rows_beyond_the_range_of_mean_times_rstd(shape, weights):
+    """h - mean is zero in every channel, and what lanes without channels hold in its place does not count."""
+    from paper_2605_08962_amd import binding
+    x = torch.full(shape, 3.5e25, device="cuda").to(torch.bfloat16)
+    x[1], x[2], x[3] = -1e30, 1.0, 0.0
+    w = (1 + 0.1 * B.bf(shape[-1], seed=2).float()) if weights else None
+    f = binding.varlen_attn_norm_fwd(x, w, eps=1e-30)
+    dy = B.bf(*shape, seed=4)
+    got = binding.varlen_attn_norm_bwd(dy, x, f.mean, f.rstd, w)
+    (dx, dx_off), _, (db, db_off) = B.norm_bwd(dy, x, f.mean, f.rstd, w, None)
+    assert _finite(f.mean, f.rstd, *got)
+    B.assert_within("dx", got[0], dx, dx_off)
+    if w is not None:
+        assert not got[1].any()
+        B.assert_within("db", got[2], db, db_off)
