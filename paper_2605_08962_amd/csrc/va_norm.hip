@@ -278,22 +278,28 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
         const int64_t flat = place.flat, out_at = place.at[2];
         const bool there = place.row < a.rows;
         Row now = next;
-        // n = (h - mean) rstd, dy and g = dy w of run j; `plain`: h - mean in place of n, where the row is in bf16.  Formed twice, for
-        // the sums and for dx: kept, they would be 24 registers a run instead of 8 or 6, which is a wave per SIMD or two.  In 8 bits n
-        // is one product and sum from the code.  Behind the row's end dy, and so g, is zero, and n is no infinity (mean rstd may be one).
+        // n = (h - mean) rstd, dy and g = dy w of run j; `plain`: h - mean in place of n.  Formed twice, for the sums and for dx: kept,
+        // they would be 24 registers a run instead of 8 or 6, which is a wave per SIMD or two.  In 8 bits h - mean is one product and sum
+        // from the code, rounded once; never code (scale rstd) - mean rstd, whose parts are beyond fp32 for rows that are far off zero and
+        // hardly vary, and whose difference loses what the row's distance from zero takes of fp32.  Behind the row's end dy, and so g, is
+        // zero, and n is no infinity (mean rstd may be one).
         auto run = [&](int j, bool plain, float* n, float* dy, float* g) {
             const int left = C - 8 * (lane + j * G);
-            const float rstd = MODE == RAGGED || left > 0 ? now.rstd : 0.f;
             if constexpr (FORMAT < 0) {
                 to_float8(now.x[j], n);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) n[e] = plain ? n[e] - now.mean : (n[e] - now.mean) * rstd;
+                for (int e = 0; e < 8; ++e) n[e] -= now.mean;
             } else {
-                act8_decode(now.codes[j], now.scale[j] * rstd, FORMAT, n, now.mean * rstd);
+                act8_decode(now.codes[j], now.scale[j], FORMAT, n, now.mean);
             }
-            if (MODE == RAGGED && !plain && left < 8) {
+            if (!plain) {
+                const float rstd = MODE == RAGGED || left > 0 ? now.rstd : 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) n[e] = e < left ? n[e] : 0.f;
+                for (int e = 0; e < 8; ++e) n[e] *= rstd;
+                if (MODE == RAGGED && left < 8) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) n[e] = e < left ? n[e] : 0.f;
+                }
             }
             to_float8(now.dy[j], dy);
             u.weight.get(j, lane, g);
@@ -326,7 +332,7 @@ __global__ void __launch_bounds__(RowGroup<G>::THREADS) norm_bwd_kernel(NormArgs
         row_sum<G>(sum, lds, at);
         // dx = rstd (g - n sum(g n) / C) - rstd sum g / C.  (rstd^2, which the other order forms from h - mean, is beyond fp32 for rows of
         // next to no variance.)
-        const float cn = -(sum[1] * inv_c), c1 = FORMAT < 0 ? now.rstd * cn : cn, c0 = -now.rstd * (sum[0] * inv_c);
+        const float c1 = -now.rstd * (sum[1] * inv_c), c0 = -now.rstd * (sum[0] * inv_c);
         uint16_t* const out = (uint16_t*)a.dx + out_at;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {  // (the compiler must not see that it has formed them before)
