@@ -449,6 +449,11 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _if_on_gpu(t):
+    """A caller's own buffer, or None for one in pinned host memory (see _require_room), which is on no GPU."""
+    return t if t is not None and t.is_cuda else None
+
+
 def _token_stride(t, name, dims=(3,)):
     """Elements from one token to the next of a bf16 tensor [T, H, D] (or [T, C]) on the GPU, whose channels (and heads) lie side by
     side: contiguous, or a part of a wider tensor."""
@@ -659,7 +664,8 @@ def varlen_attn_bwd_act8(dout, q, k, v, out, lse, cu_seqlens, causal, softmax_sc
         _require_room(t, torch.bfloat16, n, shape.numel())
     _require_room(workspace, None, "workspace")
     p = _params_of(q.codes, k.codes, cu_seqlens, causal, softmax_scale, kv_splits, max_seqlen)
-    with _On(dout, stream, q=q.codes, k=k.codes, v=v.codes, out=out.codes, lse=lse, cu_seqlens=cu_seqlens) as on:
+    with _On(dout, stream, q=q.codes, k=k.codes, v=v.codes, out=out.codes, lse=lse, cu_seqlens=cu_seqlens, dq=_if_on_gpu(dq),
+             dk=_if_on_gpu(dk), dv=_if_on_gpu(dv), workspace=_if_on_gpu(workspace)) as on:
         dq = on.empty(qs, torch.bfloat16) if dq is None else dq
         dk = on.empty(ks, torch.bfloat16) if dk is None else dk
         dv = on.empty(ks, torch.bfloat16) if dv is None else dv
@@ -780,7 +786,7 @@ def varlen_attn_norm_bwd(dy, x, mean, rstd, weight=None, dsummed=None, dx=None, 
     p = _norm_params(shape, _check_weights(weight, None, shape[-1]), number, 0.0, x_stride, dy_stride, dx_stride)
     codes, scales = x if packed else (None, None)
     with _On(dy, stream, x=x.codes if packed else x, mean=mean, rstd=rstd, weight=weight, dsummed=dsummed, dx=dx, dweight=dweight,
-             dbias=dbias) as on:
+             dbias=dbias, workspace=_if_on_gpu(workspace)) as on:
         dx = on.empty(shape, torch.bfloat16) if dx is None else dx
         if weight is not None:
             dweight = on.empty(shape[-1:], torch.float32) if dweight is None else dweight
