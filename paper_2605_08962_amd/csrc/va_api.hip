@@ -564,7 +564,7 @@ int rotary_impl(const varlen_attn_rotary_params* p, const void* q, const void* k
     if (p->head_dim < 2 || p->head_dim > 512) return VA_ERR_UNSUPPORTED;
     const int64_t qw = (int64_t)p->num_q_heads * p->head_dim, kw = (int64_t)p->num_kv_heads * p->head_dim;
     // (a token's items are counted in 32 bits, eight tokens at a time)
-    if (2 * p->num_pairs > p->head_dim || qw + 2 * kw > INT32_MAX / 16 || p->q_stride < qw || p->q_out_stride < qw ||
+    if (p->num_pairs > p->head_dim / 2 || qw + 2 * kw > INT32_MAX / 16 || p->q_stride < qw || p->q_out_stride < qw ||
         p->k_stride < kw || p->k_out_stride < kw || ((v || v_out) && (p->v_stride < kw || p->v_out_stride < kw)))
         return VA_ERR_BAD_SHAPE;
     if (p->total_tokens == 0) return VA_OK;
