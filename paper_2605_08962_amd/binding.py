@@ -454,12 +454,20 @@ def _if_on_gpu(t):
     return t if t is not None and t.is_cuda else None
 
 
+def _require_32_bits(**sizes):
+    """Sizes go to the library as 32-bit numbers, into which ctypes puts the low half of a larger one without a word."""
+    for name, n in sizes.items():
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise ValueError(f"{name} must be below 2^31")
+
+
 def _token_stride(t, name, dims=(3,)):
     """Elements from one token to the next of a bf16 tensor [T, H, D] (or [T, C]) on the GPU, whose channels (and heads) lie side by
     side: contiguous, or a part of a wider tensor."""
     if not (t.is_cuda and t.dtype == torch.bfloat16 and t.dim() in dims):
         raise ValueError(f"{name} must be a torch.bfloat16 tensor of {' or '.join(map(str, dims))} dimensions on the GPU")
     shape, strides = t.shape, t.stride()
+    _require_32_bits(**{f"{name}'s every size": max(shape)})
     width = shape[1] if t.dim() == 2 else shape[1] * shape[2]
     if t.numel() == 0:
         return width
@@ -487,6 +495,7 @@ def varlen_attn_rotary_positions(cu_rows, grids, total_tokens, first=None, merge
         if t is not None:
             _require(t, torch.int32, n)
     segments = cu_rows.numel() - 1
+    _require_32_bits(total_tokens=int(total_tokens), merge=int(merge), **{"cu_rows' size": segments})
     if cu_rows.dim() != 1 or segments < 0 or tuple(grids.shape) != (segments, 3):
         raise ValueError("grids must be [S, 3] for the S + 1 elements of cu_rows")
     if first is not None and first.numel() != segments:
@@ -519,6 +528,7 @@ def _rotary(inverse, names, q, k, v, positions, inv_freq, pair_axis, interleaved
         raise ValueError("positions must be [axes, T]")
     if inv_freq.dim() != 1 or pair_axis.shape != inv_freq.shape:
         raise ValueError("pair_axis must match inv_freq")
+    _require_32_bits(axes=positions.shape[0], pairs=inv_freq.numel())
     for (n, t), like in zip(outs.items(), (q, k, v)):
         if t is not None:
             _out_like(t, like.shape, n)
@@ -562,6 +572,7 @@ def _check_act8(x, name):
     codes, scales = x
     if not (codes.is_cuda and codes.dtype in _ACT8_OF_TYPE and codes.is_contiguous() and codes.dim() in (2, 3)):
         raise ValueError(f"{name}.codes must be a contiguous torch.int8 or torch.float8_e4m3fn tensor of 2 or 3 dimensions on the GPU")
+    _require_32_bits(**{f"{name}.codes' every size": max(codes.shape)})
     _require(scales, torch.float32, f"{name}.scales")
     if tuple(scales.shape) != _act8_shape(codes.shape) or scales.device != codes.device:
         raise ValueError(f"{name}.scales must be {_act8_shape(codes.shape)} on {codes.device}")
@@ -663,7 +674,8 @@ def varlen_attn_bwd_act8(dout, q, k, v, out, lse, cu_seqlens, causal, softmax_sc
     for t, shape, n in ((dq, qs, "dq"), (dk, ks, "dk"), (dv, ks, "dv")):
         _require_room(t, torch.bfloat16, n, shape.numel())
     _require_room(workspace, None, "workspace")
-    p = _params_of(q.codes, k.codes, cu_seqlens, causal, softmax_scale, kv_splits, max_seqlen)
+    _require_32_bits(kv_splits=int(kv_splits), **{"cu_seqlens' size": cu_seqlens.numel()})
+    p = _params_of(q.codes, k.codes, cu_seqlens, causal, softmax_scale, kv_splits, min(int(max_seqlen), 2 ** 31 - 1))
     with _On(dout, stream, q=q.codes, k=k.codes, v=v.codes, out=out.codes, lse=lse, cu_seqlens=cu_seqlens, dq=_if_on_gpu(dq),
              dk=_if_on_gpu(dk), dv=_if_on_gpu(dv), workspace=_if_on_gpu(workspace)) as on:
         dq = on.empty(qs, torch.bfloat16) if dq is None else dq
