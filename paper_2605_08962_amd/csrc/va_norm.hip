@@ -104,25 +104,25 @@ struct Weights {
 template <int N>
 struct RowPlace {
     int64_t row, flat, at[N];
-    int inner;  // which of its token's rows
+    uint32_t inner;  // which of its token's rows
 };
 template <int N>
 struct RowWalk {
     int64_t step, by_flat, by[N], wrap[N];
-    int by_inner, rows_per_token;
+    uint32_t by_inner, rows_per_token;  // (unsigned: up to 2^31 - 1 rows a token and a step's rows do not fit 31 bits together)
     // step and first are below 2^31: rows of one round of the grid
     __device__ __forceinline__ RowPlace<N> begin(const NormArgs& a, int64_t first, int64_t step_, const int64_t (&stride)[N]) {
         const uint32_t rpt = (uint32_t)a.rows_per_token, f = (uint32_t)first, s = (uint32_t)step_;
         const uint32_t token = rpt == 1 ? f : f / rpt, tokens = rpt == 1 ? s : s / rpt;
         const int C = a.channels;
-        rows_per_token = (int)rpt;
+        rows_per_token = rpt;
         step = step_;
         by_flat = step * C;
-        by_inner = (int)(s - tokens * rpt);
+        by_inner = s - tokens * rpt;
         RowPlace<N> p;
         p.row = first;
         p.flat = first * C;
-        p.inner = (int)(f - token * rpt);
+        p.inner = f - token * rpt;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             p.at[i] = token * stride[i] + (int64_t)p.inner * C;
