@@ -15,12 +15,13 @@ constexpr int ACT8_THREADS = 256;
 template <int G, int U, int MODE, bool PACK>
 __global__ void __launch_bounds__(ACT8_THREADS) act8_kernel(Act8Args a) {
     constexpr int GROUPS = ACT8_THREADS / G;
+    const uint32_t wg = a.first_wg + blockIdx.x;
     int ti = 0;
-    while (ti + 1 < a.num && blockIdx.x >= a.t[ti + 1].first_wg) ++ti;
+    while (ti + 1 < a.num && wg >= a.t[ti + 1].first_wg) ++ti;
     const Act8Tensor& x = a.t[ti];
     const int lane = threadIdx.x % G;
     const int blocks = (x.channels + kAct8Block - 1) / kAct8Block;
-    const int64_t groups = x.rows * blocks, first = (int64_t)(blockIdx.x - x.first_wg) * (GROUPS * U) + threadIdx.x / G;
+    const int64_t groups = x.rows * blocks, first = (int64_t)(wg - x.first_wg) * (GROUPS * U) + threadIdx.x / G;
     int64_t row[U];
     int block[U], n[U];  // n: channels from this lane's on (lanes without any keep the others company)
     uint16_t* v[U];
@@ -88,23 +89,24 @@ static hipError_t launch_act8(Act8Args a, hipStream_t stream) {
         const int64_t groups = a.t[i].rows * ((a.t[i].channels + kAct8Block - 1) / kAct8Block);
         wgs += (groups + per_wg - 1) / per_wg;
     }
-    if (wgs == 0) return hipSuccess;
     if (wgs > INT32_MAX) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)wgs), block(ACT8_THREADS);
     const bool stream_past = bytes > (int64_t)256 << 20;  // beyond the last-level cache nothing is found there again
+    return launch_in_parts(wgs, [&](uint32_t first, unsigned n) {
+        const dim3 grid(n), block(ACT8_THREADS);
+        a.first_wg = first;
 #define VA_ACT8(G, U, MODE) hipLaunchKernelGGL((act8_kernel<G, U, MODE, PACK>), grid, block, 0, stream, a)
 #define VA_ACT8_MODE(G, U)                           \
     if (!wide) VA_ACT8(G, U, RAGGED);                \
     else if (stream_past) VA_ACT8(G, U, STREAM);     \
     else VA_ACT8(G, U, WIDE);
-    if (G == 8) {
-        if (full) { VA_ACT8_MODE(8, 2) } else { VA_ACT8_MODE(8, 4) }
-    } else {
-        if (full) { VA_ACT8_MODE(16, 2) } else { VA_ACT8_MODE(16, 4) }
-    }
+        if (G == 8) {
+            if (full) { VA_ACT8_MODE(8, 2) } else { VA_ACT8_MODE(8, 4) }
+        } else {
+            if (full) { VA_ACT8_MODE(16, 2) } else { VA_ACT8_MODE(16, 4) }
+        }
 #undef VA_ACT8_MODE
 #undef VA_ACT8
-    return hipGetLastError();
+    });
 }
 
 hipError_t launch_act8_pack(const Act8Args& a, hipStream_t stream) { return launch_act8<true>(a, stream); }

@@ -141,6 +141,19 @@ hipError_t launch_merge(const void* o_parts, bool parts_fp32, const float* lse_p
 hipError_t launch_bwd_dkdv(const BwdArgs& a, hipStream_t stream);
 hipError_t launch_bwd_dq(const BwdArgs& a, hipStream_t stream);
 
+// A launch has fewer than 2^32 threads (HIP's limit, of 256 a workgroup here): work for more goes in parts, launch(first, wgs) one after
+// the other, first being added to the workgroup's number.
+template <typename F>
+hipError_t launch_in_parts(int64_t wgs, F launch) {
+    constexpr int64_t MOST = ((int64_t)1 << 24) - 1;
+    for (int64_t first = 0; first < wgs; first += MOST) {
+        launch((uint32_t)first, (unsigned)(wgs - first < MOST ? wgs - first : MOST));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // Rotary positions (va_rotary.hip).  Strides in elements between tokens; the channels of a token's heads lie side by side.
 struct RotaryArgs {
     const uint16_t *q, *k, *v;  // bf16; v may be null
@@ -155,6 +168,7 @@ struct RotaryArgs {
     struct Divisor { uint32_t factor, shift; } by_token, by_head, by_v, by_pairs;
     int per_token, per_head, per_v;  // items of a token, a head of q or k, a head of v
     int tile, tile_tokens;           // items and tokens of a workgroup
+    uint32_t first_wg;               // of this launch
 };
 hipError_t launch_rotary(RotaryArgs a, hipStream_t stream);
 hipError_t launch_rotary_positions(int total_tokens, int num_segments, int merge, const int32_t* cu, const int32_t* grids,
@@ -193,6 +207,7 @@ constexpr int ACT8_MAX_TENSORS = 8;
 struct Act8Args {
     Act8Tensor t[ACT8_MAX_TENSORS];
     int num, format;
+    uint32_t first_wg;  // of this launch (filled by it)
 };
 hipError_t launch_act8_pack(const Act8Args& a, hipStream_t stream);
 hipError_t launch_act8_unpack(const Act8Args& a, hipStream_t stream);

@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
     typedef typename RotaryVec<VEC>::type Vec;
     typedef typename RotaryVec<VEC>::any VecAny;
     const int P = a.num_pairs, D = a.head_dim;
-    const int64_t t0 = (int64_t)blockIdx.x * a.tile_tokens;
+    const int64_t t0 = (int64_t)(a.first_wg + blockIdx.x) * a.tile_tokens;
     const int nt = (int)min((int64_t)a.tile_tokens, a.total_tokens - t0);
     const int turned = P / VEC;                     // items of a head that turn; then those that are copied
     const int nq = a.num_q_heads * a.per_head, nqk = nq + a.num_kv_heads * a.per_head;
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_flat_kernel(RotaryArgs a) 
     constexpr bool INTERLEAVED = PARTNER == HERE;
     extern __shared__ float angles[];  // cos [tile_tokens][P], then sin
     const int P = a.num_pairs;
-    const int64_t f0 = (int64_t)blockIdx.x * a.tile, total = (int64_t)a.total_tokens * a.per_token;
+    const int64_t f0 = (int64_t)(a.first_wg + blockIdx.x) * a.tile, total = (int64_t)a.total_tokens * a.per_token;
     const int64_t t0 = f0 / a.per_token;
     const int r0 = (int)(f0 - t0 * a.per_token), n = (int)min((int64_t)a.tile, total - f0);
     const int nq = a.num_q_heads * a.per_head, nqk = nq + a.num_kv_heads * a.per_head;
@@ -327,23 +327,25 @@ hipError_t launch_rotary(RotaryArgs a, hipStream_t stream) {
         a.by_head = divisor(a.per_head);
         const int64_t runs = (int64_t)a.total_tokens * a.per_token, wgs = (runs + a.tile - 1) / a.tile;
         if (wgs > INT32_MAX) return hipErrorInvalidConfiguration;
-        const dim3 grid((unsigned)wgs);
         const size_t lds = 2 * sizeof(float) * a.tile_tokens * a.num_pairs;
         const bool streamed = runs * 32 > (int64_t)256 << 20;  // beyond the last-level cache nothing is found there again
         const bool whole = a.head_dim == 2 * a.num_pairs;
         const int partner = a.interleaved ? HERE : whole && a.num_pairs == 32 ? LANE4 : whole && a.num_pairs == 64 ? LANE8 : MEMORY;
+        return launch_in_parts(wgs, [&](uint32_t first, unsigned n) {
+            const dim3 grid(n);
+            a.first_wg = first;
 #define VA_ROTARY(PARTNER)                                                                                               \
     if (streamed) hipLaunchKernelGGL((rotary_flat_kernel<PARTNER, true>), grid, block, lds, stream, a);                  \
     else hipLaunchKernelGGL((rotary_flat_kernel<PARTNER, false>), grid, block, lds, stream, a);                          \
     break;
-        switch (partner) {
-            case HERE: VA_ROTARY(HERE)
-            case LANE4: VA_ROTARY(LANE4)
-            case LANE8: VA_ROTARY(LANE8)
-            default: VA_ROTARY(MEMORY)
-        }
+            switch (partner) {
+                case HERE: VA_ROTARY(HERE)
+                case LANE4: VA_ROTARY(LANE4)
+                case LANE8: VA_ROTARY(LANE8)
+                default: VA_ROTARY(MEMORY)
+            }
 #undef VA_ROTARY
-        return hipGetLastError();
+        });
     }
     const int vec = (a.head_dim | a.num_pairs) % 4 == 0 ? 4 : 1;  // the widest run that divides both
     a.tile_tokens = a.total_tokens >= 4096 ? 4 : 1;
@@ -353,13 +355,15 @@ hipError_t launch_rotary(RotaryArgs a, hipStream_t stream) {
     a.by_token = divisor(a.per_token);
     a.by_head = divisor(a.per_head);
     a.by_v = divisor(a.per_v);
-    const dim3 grid((unsigned)((a.total_tokens + (int64_t)a.tile_tokens - 1) / a.tile_tokens));
     const size_t lds = 2 * sizeof(float) * a.tile_tokens * a.num_pairs;
-    if (vec == 4 && a.interleaved) hipLaunchKernelGGL((rotary_kernel<4, true>), grid, block, lds, stream, a);
-    else if (vec == 4) hipLaunchKernelGGL((rotary_kernel<4, false>), grid, block, lds, stream, a);
-    else if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<1, true>), grid, block, lds, stream, a);
-    else hipLaunchKernelGGL((rotary_kernel<1, false>), grid, block, lds, stream, a);
-    return hipGetLastError();
+    return launch_in_parts((a.total_tokens + (int64_t)a.tile_tokens - 1) / a.tile_tokens, [&](uint32_t first, unsigned n) {
+        const dim3 grid(n);
+        a.first_wg = first;
+        if (vec == 4 && a.interleaved) hipLaunchKernelGGL((rotary_kernel<4, true>), grid, block, lds, stream, a);
+        else if (vec == 4) hipLaunchKernelGGL((rotary_kernel<4, false>), grid, block, lds, stream, a);
+        else if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<1, true>), grid, block, lds, stream, a);
+        else hipLaunchKernelGGL((rotary_kernel<1, false>), grid, block, lds, stream, a);
+    });
 }
 
 }  // namespace va
