@@ -202,10 +202,10 @@ int varlen_attn_check_cu_seqlens(const varlen_attn_params *p, const int32_t *cu_
  * What runs around attention in a block's training step, on the same packed tokens: rotary positions, layer norm, and
  * checkpoints of activations in 8 bits.  All calls obey the contract at the top of this file (device pointers, nothing allocated
  * or synchronised, capturable, every host-visible argument checked before anything is enqueued), except that their tensors need
- * no more alignment than their elements have: rows that start on 16-byte boundaries and hold a multiple of 8 channels are moved 16
- * bytes at a time, others element by element, with the same results.  Strides are in elements, from one token to the next, and a token's
- * heads and channels lie side by side: a tensor may be a part of a wider one, such as q inside the fused projection
- * [T, Hq + 2 Hkv, D].  Unless said otherwise no output may overlap an input or another output.
+ * no more alignment than their elements have: eight channels are moved by one 16-byte access at whatever address they start, what is
+ * left of a row by smaller ones, with the same results.  Strides are in elements, from one token to the next, and a token's heads and
+ * channels lie side by side: a tensor may be a part of a wider one, such as q inside the fused projection [T, Hq + 2 Hkv, D].  Unless
+ * said otherwise no output may overlap an input or another output.
  */
 
 /*
@@ -229,8 +229,9 @@ int varlen_attn_rotary_positions(int32_t total_tokens, int32_t num_segments, int
  * where (x1, x2) are channels (j, j + num_pairs), or (2j, 2j + 1) if interleaved.  Channels from 2 num_pairs on are copied, and so
  * is v if it is given: q, k and v come out of the fused projection as the contiguous tensors that varlen_attn_fwd reads.
  * varlen_attn_rotary_bwd turns by -phi: q, k, v are then the gradients of the forward's outputs and q_out, k_out, v_out those of its
- * inputs, which may be parts of the fused projection's gradient.  Angles are formed in 64 bits (any position's is right to
- * 2^-20), the rotation in fp32, results are rounded to bf16 once.
+ * inputs, which may be parts of the fused projection's gradient.  Angles are formed in 64 bits: right to
+ * 2^-20 up to |position * inv_freq| = 2^31, beyond it to 2^-51 of that product.  The rotation is in fp32, results are rounded to bf16
+ * once.
  *   q, q_out   bf16 [T, num_q_heads,  head_dim];  k, k_out, v, v_out bf16 [T, num_kv_heads, head_dim]; v and v_out both or neither
  *   positions  DEVICE int32 [num_axes, total_tokens];  inv_freq  DEVICE fp32 [num_pairs], finite
  *   pair_axis  DEVICE int32 [num_pairs], each in [0, num_axes); others are taken as the nearest axis

@@ -14,7 +14,8 @@ namespace va {
 constexpr int ROT_THREADS = 256;
 
 // cos and sin of a position's angle.  The angle of a far position does not fit 32 bits (2^20 at frequency 1 leaves steps of 1/16):
-// it is reduced to turns in 64 bits, of which the fraction is taken, and the rest is 32-bit work.
+// it is reduced to turns in 64 bits, of which the fraction is taken, and the rest is 32-bit work.  The two products and the constant are
+// each off by half a step, 3 * 2^-53 of the angle together: under 2^-20 with the 32-bit part up to 2^31, 2^-51 of the angle beyond.
 __device__ __forceinline__ void rotary_angle(int position, float inv_freq, float& c, float& s) {
     const double turns = (double)position * (double)inv_freq * 0.15915494309189535;  // 1 / (2 pi)
     sincospif(2.f * (float)(turns - __builtin_rint(turns)), &s, &c);
