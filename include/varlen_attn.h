@@ -299,7 +299,8 @@ int varlen_attn_bwd_act8(const varlen_attn_params *p, int32_t format, const void
  *     dx = rstd (g - sum g / C - n sum(g n) / C) + dsummed,   dweight = sum over rows of dy n,   dbias = sum over rows of dy
  * from h in bf16 (x) or in 8 bits (x NULL, codes and scales as the forward left them).  dx is the gradient of x and of residual; dsummed,
  * the gradient that reaches `summed` on its own way, may be NULL.  dweight and dbias are fp32 and written if weight is given (all
- * zeros where there are no rows).  Statistics and sums are fp32; the same call gives the same bits.
+ * zeros where there are no rows).  Statistics and sums are fp32: a row whose squares about its mean add up to
+ * 2^128 or more has no result.  The same call gives the same bits.
  *   x, y, dy, dx, residual, summed, dsummed  bf16;   mean, rstd  fp32 [total_tokens, rows_per_token]
  *   Only x, dy and dx have strides; the others lie row by row.
  */

@@ -426,7 +426,10 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* __restrict_
 //   65536 x 2048    5.39 5.98 5.69 5.76 5.84 / 4.80 5.71 5.06 5.49 5.12        32768 x 4096   3.52 5.80 5.94 5.54 5.49 / 3.32 5.27 5.31 4.42 4.46
 //   32768 x 32 heads of 128   2.32 3.88 5.13 5.58 4.73 / 2.61 4.47 5.43 5.45 5.38        16000 x 8000   4.46 5.60 4.76 5.33 4.93 / 5.27 4.96 4.54 4.26 3.40
 //   8000 x 16000    5.60 5.37 5.17 4.90 4.15 / 4.95 4.21 3.71 3.32 2.27
-// (the backward's registers allow two at 1280 channels: with three the third waits).  A forward that leaves codes has more to do between
+// (the backward's registers allow two at 1280 channels: with three the third waits; of 512 threads for more than 8192 they allow one, and
+// 3 to 7 of them go to scratch).  Rows just above a limit leave lanes or runs empty at the same number of workgroups, so fewer bytes are in
+// flight: 520 channels 3.6 / 3.9 TB/s, 640 4.4 / 4.7, 1032 5.4 / 5.3, 2056 3.5 / 3.4, 2560 4.3 / 4.2, 4104 4.4 / 3.3, 5120 5.6 / 4.1, 8200
+// 4.8 / 4.2.  A forward that leaves codes has more to do between
 // a row's arrival and its end, and takes one more: 65537 x 1280 5.36 -> 5.63, 65536 x 2048 5.80 -> 6.30 (two runs a thread: 6.24 -> 5.81).
 #define VA_NORM_SHAPES(GO) \
     if (C <= 64) GO(8, 1, 4, 4) else if (C <= 128) GO(16, 1, 4, 4) else if (C <= 256) GO(32, 1, 4, 4) else if (C <= 512) GO(64, 1, 4, 4) \
